@@ -324,8 +324,9 @@ st_status st_tensor_shape(const st_net* net, int32_t layer, int32_t* nhwc);
 
 void st_destroy_net(st_net* net);
 
-/* Message of the last failure on `net` (or of the calling thread's last
- * st_create_net failure when net is NULL).  Owned by the library. */
+/* Message of the last failure on `net` (when net is NULL: of the calling
+ * thread's last failure of a call that takes no net, or of creating one).
+ * Owned by the library. */
 const char* st_last_error(const st_net* net);
 
 /* ---- parity / introspection: host copies of the last frame's artefacts
@@ -407,6 +408,166 @@ st_status st_profile_begin(st_net* net, int32_t max_launches,
 st_status st_profile_end(st_net* net, st_launch_record* recs, int32_t cap,
                          int32_t* n, int64_t* counts, int32_t cap_frames,
                          int32_t* n_frames);
+
+/* ---- operators behind the encoder: what a recurrent video model (the
+ * paper's CRNN, a CNN encoder followed by a recurrent part) does with the
+ * encoder's maps.  Forward and backward calls on plain tensors; no st_net.
+ *
+ * As everywhere in this library, the caller owns all memory: a call takes a
+ * device workspace of at least the bytes its *_workspace call reports
+ * (256-byte aligned; NULL when it reports 0), whose contents need not be
+ * initialised and mean nothing afterwards.  Calls are asynchronous on
+ * `stream`, which belongs to the current device, as all memory does; they
+ * allocate nothing, never wait, keep no state, may be captured into a HIP
+ * graph, and may run from several threads and on several streams at once
+ * with a workspace each.  Results do not vary from run to run.  On failure
+ * st_last_error(NULL) has the calling thread's message and nothing was
+ * launched (ST_ERR_HIP aside).
+ *
+ * Outputs must not overlap inputs, the workspace or one another, except
+ * where a call says so.  Data type pairs (dtype, out_dtype): equal ones, and
+ * ST_F32 with any; `dtype` is that of the inputs and of their gradients,
+ * `out_dtype` that of the output and of its gradient.  Parameters,
+ * statistics and the recurrent state are f32, and so is all arithmetic;
+ * results are rounded once, to nearest even. */
+
+/* A channels-last map [n][h][w][c]: strides in elements, channels adjacent.
+ * An output's elements must not overlap. */
+typedef struct st_map_ref {
+  void* data;
+  int64_t stride_n, stride_h, stride_w;
+} st_map_ref;
+
+/* Group norm with an activation.  groups divides c.  act: ST_ACT_*.  n may
+ * be 0; h, w, c at least 1. */
+typedef struct st_norm_desc {
+  int32_t dtype, out_dtype;
+  int32_t n, h, w, c, groups, act;
+  float eps; /* >= 0 */
+} st_norm_desc;
+
+/* Workspace of st_group_norm (backward = 0) or st_group_norm_backward (1).
+ * Host only.  Errors: ST_ERR_INVALID_ARG. */
+st_status st_group_norm_workspace(const st_norm_desc* d, int32_t backward,
+                                  uint64_t* bytes);
+
+/* y = act((x - mean) * rstd * gamma[c] + beta[c]) with, per image and group
+ * of c / groups adjacent channels, the mean and rstd = 1 / sqrt(var + eps)
+ * (biased variance) over the group's channels and all sites.  gamma, beta:
+ * [c], NULL for 1 and 0.  mean, rstd: [n][groups], written for
+ * st_group_norm_backward; both or neither may be NULL.  y may be x itself
+ * (the same address, strides and type).
+ * Errors: ST_ERR_INVALID_ARG, ST_ERR_WORKSPACE, ST_ERR_HIP. */
+st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
+                        const float* gamma, const float* beta,
+                        const st_map_ref* y, float* mean, float* rstd,
+                        void* ws, uint64_t ws_bytes, void* stream);
+
+/* Gradients of st_group_norm from dy (out_dtype) and the forward call's x,
+ * mean, rstd, gamma and beta: dx (dtype; may be x itself, or dy itself where
+ * dtype == out_dtype), dgamma and dbeta ([c], summed over images and sites;
+ * either may be NULL).  Errors as st_group_norm. */
+st_status st_group_norm_backward(const st_norm_desc* d, const st_map_ref* dy,
+                                 const st_map_ref* x, const float* mean,
+                                 const float* rstd, const float* gamma,
+                                 const float* beta, const st_map_ref* dx,
+                                 float* dgamma, float* dbeta, void* ws,
+                                 uint64_t ws_bytes, void* stream);
+
+/* A sequence tensor [t][b][c] (time, rows, channels): strides in elements,
+ * channels adjacent.  An output's elements must not overlap.  The frames of
+ * a chunk are such a tensor as st_encode_chunk leaves them, with one row per
+ * image and site. */
+typedef struct st_seq_ref {
+  void* data;
+  int64_t stride_t, stride_b;
+} st_seq_ref;
+
+/* The axes of a sequence operator.  t and b may be 0; c at least 1; b * c
+ * below 2^31.
+ *   lengths  device int32 [b], or NULL (every row has t steps): row i has
+ *            lengths[i] steps (values outside [0, t] count as the nearer
+ *            bound).  What lies behind them is not read; outputs behind
+ *            them are zero.
+ *   reset    device uint8 [t][b], or NULL: at a non-zero entry the row
+ *            forgets everything before that step (a new chunk, a cut, the
+ *            next of several sequences packed into one row).
+ *   reverse  non-zero: rows run from their last step to their first.
+ * "Before" and "next" below are meant in the order in which a row runs. */
+typedef struct st_seq_desc {
+  int32_t dtype, out_dtype;
+  int32_t t, b, c;
+  int32_t reverse;
+  const int32_t* lengths;
+  const uint8_t* reset;
+} st_seq_desc;
+
+#define ST_TIME_CONV_MAX_TAPS 8
+
+st_status st_time_conv_workspace(const st_seq_desc* d, int32_t taps,
+                                 int32_t backward, uint64_t* bytes);
+
+/* Causal depthwise convolution along time with an activation:
+ * y_s = act(bias[c] + sum_j weight[j][c] * x_{s - taps + 1 + j}), j in
+ * [0, taps), taps in [1, ST_TIME_CONV_MAX_TAPS].  weight: [taps][c]; bias:
+ * [c] or NULL.  window: the taps - 1 inputs before the first step, oldest
+ * first, dtype, [taps - 1][b][c] contiguous, or NULL (zeros).  window_out:
+ * receives the last taps - 1 inputs of every row (zeros for those that a
+ * reset hides), which the next call over the same rows takes as its window;
+ * may be NULL, and may be `window` itself.
+ * Errors: ST_ERR_INVALID_ARG, ST_ERR_WORKSPACE, ST_ERR_HIP. */
+st_status st_time_conv(const st_seq_desc* d, int32_t taps, int32_t act,
+                       const st_seq_ref* x, const float* weight,
+                       const float* bias, const void* window,
+                       const st_seq_ref* y, void* window_out, void* ws,
+                       uint64_t ws_bytes, void* stream);
+
+/* Gradients of st_time_conv from dy (out_dtype) and the forward call's
+ * inputs: dx, dweight [taps][c], dbias [c], dwindow (as window).
+ * dwindow_out: the gradient with respect to window_out (dtype, NULL: zero).
+ * dx, dweight, dbias and dwindow may be NULL.  Errors as st_time_conv. */
+st_status st_time_conv_backward(const st_seq_desc* d, int32_t taps,
+                                int32_t act, const st_seq_ref* dy,
+                                const st_seq_ref* x, const float* weight,
+                                const float* bias, const void* window,
+                                const void* dwindow_out,
+                                const st_seq_ref* dx, float* dweight,
+                                float* dbias, void* dwindow, void* ws,
+                                uint64_t ws_bytes, void* stream);
+
+/* Steps between the states that st_gated_scan keeps for its backward pass. */
+#define ST_SCAN_STRIDE 16
+
+st_status st_gated_scan_workspace(const st_seq_desc* d, int32_t backward,
+                                  uint64_t* bytes);
+
+/* Gated linear recurrence, per row and channel:
+ *   h_s = sigmoid(f_s) * h_{s-1} + sigmoid(-f_s) * v_s
+ *   y_s = h_s * sigmoid(o_s)          (y_s = h_s where o is NULL)
+ * h: the state before the first step, f32 [b][c], or NULL (zeros).  h_out:
+ * receives the state after each row's last step, f32 [b][c]; may be NULL,
+ * and may be `h` itself.  states: f32 [ceil(t / ST_SCAN_STRIDE)][b][c], or
+ * NULL: receives the state before steps 0, ST_SCAN_STRIDE, ... for
+ * st_gated_scan_backward (entries behind a row's length are left as they
+ * were).  Errors: ST_ERR_INVALID_ARG, ST_ERR_WORKSPACE, ST_ERR_HIP. */
+st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
+                        const st_seq_ref* f, const st_seq_ref* o,
+                        const float* h, const st_seq_ref* y, float* h_out,
+                        float* states, void* ws, uint64_t ws_bytes,
+                        void* stream);
+
+/* Gradients of st_gated_scan from dy (out_dtype), the forward call's inputs
+ * and the states it kept: dv, df, d_o (d_o where o is given; the three may
+ * be interleaved slices of one tensor), dh (f32 [b][c], with respect to h; may
+ * be NULL).  dh_out: the gradient with respect to h_out, f32 [b][c], NULL:
+ * zero; dh may be dh_out itself.  Errors as st_gated_scan. */
+st_status st_gated_scan_backward(const st_seq_desc* d, const st_seq_ref* dy,
+                                 const st_seq_ref* v, const st_seq_ref* f,
+                                 const st_seq_ref* o, const float* states,
+                                 const float* dh_out, const st_seq_ref* dv,
+                                 const st_seq_ref* df, const st_seq_ref* d_o,
+                                 float* dh, void* ws, uint64_t ws_bytes,
+                                 void* stream);
 
 #ifdef __cplusplus
 }

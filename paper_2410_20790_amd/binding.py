@@ -39,6 +39,9 @@ EXPORTED = [
     "st_set_threshold_control", "st_encode_diff_adaptive",
     "st_get_thresholds", "st_create_net_ex", "st_debug_carry",
     "st_encode_chunk_adaptive", "st_bind_workspace_static",
+    "st_group_norm_workspace", "st_group_norm", "st_group_norm_backward",
+    "st_time_conv_workspace", "st_time_conv", "st_time_conv_backward",
+    "st_gated_scan_workspace", "st_gated_scan", "st_gated_scan_backward",
 ]
 
 
@@ -55,6 +58,28 @@ class st_layer_desc(ctypes.Structure):
         "pool_s_h", "pool_s_w", "pool_p_h", "pool_p_w", "se_mid")] + [
         (n, ctypes.c_void_p) for n in (
             "weight", "bias", "se_w1", "se_b1", "se_w2", "se_b2")]
+
+
+class st_map_ref(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_n", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("stride_w", ctypes.c_int64)]
+
+
+class st_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "dtype", "out_dtype", "n", "h", "w", "c", "groups", "act")] + [
+        ("eps", ctypes.c_float)]
+
+
+class st_seq_ref(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_t", ctypes.c_int64),
+                ("stride_b", ctypes.c_int64)]
+
+
+class st_seq_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "dtype", "out_dtype", "t", "b", "c", "reverse")] + [
+        ("lengths", ctypes.c_void_p), ("reset", ctypes.c_void_p)]
 
 
 class st_launch_record(ctypes.Structure):
@@ -111,6 +136,22 @@ def _load():
         "st_encode_chunk_adaptive": [P, P, I32, P, P],
         "st_get_thresholds": [P, ctypes.POINTER(ctypes.c_float)],
     }
+    ND, MR = ctypes.POINTER(st_norm_desc), ctypes.POINTER(st_map_ref)
+    SD, SR = ctypes.POINTER(st_seq_desc), ctypes.POINTER(st_seq_ref)
+    sig.update({
+        "st_group_norm_workspace": [ND, I32, ctypes.POINTER(U64)],
+        "st_group_norm": [ND, MR, P, P, MR, P, P, P, U64, P],
+        "st_group_norm_backward": [ND, MR, MR, P, P, P, P, MR, P, P, P, U64,
+                                   P],
+        "st_time_conv_workspace": [SD, I32, I32, ctypes.POINTER(U64)],
+        "st_time_conv": [SD, I32, I32, SR, P, P, P, SR, P, P, U64, P],
+        "st_time_conv_backward": [SD, I32, I32, SR, SR, P, P, P, P, SR, P, P,
+                                  P, P, U64, P],
+        "st_gated_scan_workspace": [SD, I32, ctypes.POINTER(U64)],
+        "st_gated_scan": [SD, SR, SR, SR, P, SR, P, P, P, U64, P],
+        "st_gated_scan_backward": [SD, SR, SR, SR, SR, P, P, SR, SR, SR, P,
+                                   P, U64, P],
+    })
     for name, args in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
@@ -337,3 +378,70 @@ def st_profile_end(net, n_layers, cap=1 << 20, cap_frames=4096):
                    dtype=[("kernel", "i4"), ("layer", "i4"), ("frame", "i4"),
                           ("ms", "f4")])
     return out, counts[:min(nf.value, cap_frames)]
+
+
+# --------------------------------------------- operators behind the encoder
+# Descriptors and tensor references are st_*_desc / st_*_ref structures (a
+# reference that may be absent: None), device addresses are integers or None.
+
+SCAN_STRIDE = 16
+TIME_CONV_MAX_TAPS = 8
+
+
+def st_group_norm_workspace(desc, backward) -> int:
+    b = ctypes.c_uint64()
+    _check(_lib.st_group_norm_workspace(desc, backward, ctypes.byref(b)))
+    return b.value
+
+
+def st_group_norm(desc, x, gamma, beta, y, mean=None, rstd=None, ws=None,
+                  ws_bytes=0, stream=0):
+    _check(_lib.st_group_norm(desc, x, gamma, beta, y, mean, rstd, ws,
+                              ws_bytes, stream))
+
+
+def st_group_norm_backward(desc, dy, x, mean, rstd, gamma, beta, dx,
+                           dgamma=None, dbeta=None, ws=None, ws_bytes=0,
+                           stream=0):
+    _check(_lib.st_group_norm_backward(desc, dy, x, mean, rstd, gamma, beta,
+                                       dx, dgamma, dbeta, ws, ws_bytes,
+                                       stream))
+
+
+def st_time_conv_workspace(desc, taps, backward) -> int:
+    b = ctypes.c_uint64()
+    _check(_lib.st_time_conv_workspace(desc, taps, backward,
+                                       ctypes.byref(b)))
+    return b.value
+
+
+def st_time_conv(desc, taps, act, x, weight, bias, window, y,
+                 window_out=None, ws=None, ws_bytes=0, stream=0):
+    _check(_lib.st_time_conv(desc, taps, act, x, weight, bias, window, y,
+                             window_out, ws, ws_bytes, stream))
+
+
+def st_time_conv_backward(desc, taps, act, dy, x, weight, bias, window,
+                          dwindow_out, dx, dweight=None, dbias=None,
+                          dwindow=None, ws=None, ws_bytes=0, stream=0):
+    _check(_lib.st_time_conv_backward(desc, taps, act, dy, x, weight, bias,
+                                      window, dwindow_out, dx, dweight,
+                                      dbias, dwindow, ws, ws_bytes, stream))
+
+
+def st_gated_scan_workspace(desc, backward) -> int:
+    b = ctypes.c_uint64()
+    _check(_lib.st_gated_scan_workspace(desc, backward, ctypes.byref(b)))
+    return b.value
+
+
+def st_gated_scan(desc, v, f, o, h, y, h_out=None, states=None, ws=None,
+                  ws_bytes=0, stream=0):
+    _check(_lib.st_gated_scan(desc, v, f, o, h, y, h_out, states, ws,
+                              ws_bytes, stream))
+
+
+def st_gated_scan_backward(desc, dy, v, f, o, states, dh_out, dv, df, d_o,
+                           dh=None, ws=None, ws_bytes=0, stream=0):
+    _check(_lib.st_gated_scan_backward(desc, dy, v, f, o, states, dh_out, dv,
+                                       df, d_o, dh, ws, ws_bytes, stream))

@@ -10,7 +10,8 @@ from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-CSRC = os.path.join(PKG, "csrc")
+CSRC = os.path.join(PKG, "csrc")          # the encoder
+OPS = os.path.join(PKG, "csrc_ops")      # the operators behind it
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsparsetem.so")
 
@@ -18,10 +19,13 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
-          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", OPS]
 # Packed-FP32 instructions are disabled for all device code.
 DEVICE = ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature",
           "-Xclang", "-packed-fp32-ops", "-munsafe-fp-atomics"]
+# The operators fuse a product and a sum where their source says so: a step
+# taken alone and in a chunk, by another kernel, has the same bits.
+EXACT = DEVICE + ["-ffp-contract=off"]
 
 SOURCES = [
     ("st_plan.cpp", []),
@@ -29,11 +33,16 @@ SOURCES = [
     ("st_dense.hip", DEVICE),
     ("st_gather.hip", DEVICE),
     ("st_exec.hip", DEVICE),
+    ("../csrc_ops/norm.hip", EXACT),
+    ("../csrc_ops/time_conv.hip", EXACT),
+    ("../csrc_ops/time_conv_grad.hip", EXACT),
+    ("../csrc_ops/gated_scan.hip", EXACT),
 ]
 
 
 def _compile(src, extra):
-    obj = os.path.join(OUT, os.path.splitext(src)[0] + ".o")
+    name = os.path.splitext(os.path.basename(src))[0]
+    obj = os.path.join(OUT, name + ".o")
     cmd = [HIPCC, *extra, *COMMON, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -1,0 +1,552 @@
+"""The operators behind the encoder against their 64-bit forms
+(ops_reference): every output within half a step of its type plus the bound
+that 32-bit arithmetic carries."""
+
+import numpy as np
+import pytest
+import torch
+
+import ops_reference as R
+from ops_reference import check, f64
+from paper_2410_20790_amd import ops
+from parity_util import say
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+PAIRS = [(F32, F32), (F16, F16), (BF16, BF16), (F32, F16), (F32, BF16)]
+
+
+def rnd(seed, *shape, dtype=F32, scale=1.0, shift=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(*shape, generator=g, dtype=torch.float64) * scale + shift
+    return x.to(dtype).cuda()
+
+
+def compare(got, want, what):
+    for name, (v, b) in want.items():
+        if name in got and got[name] is not None:
+            check(got[name], v, b, f"{what}: {name}")
+
+
+# -------------------------------------------------------------- group norm
+
+def norm_both(x, groups, gamma, beta, a, out, eps=1e-5, what="", dy=None):
+    y, mean, rstd = ops.group_norm(x, groups, gamma, beta, act=a, eps=eps,
+                                   out_dtype=out)
+    compare(dict(y=y, mean=mean, rstd=rstd),
+            R.group_norm(f64(x), groups, f64(gamma), f64(beta), a, eps), what)
+    if dy is None:
+        dy = rnd(77, *x.shape, dtype=out)
+    dx, dg, db = ops.group_norm_backward(dy, x, groups, mean, rstd, gamma,
+                                         beta, act=a)
+    if a != R.RELU:   # its kink is tested where z is exact
+        compare(dict(dx=dx, dgamma=dg, dbeta=db),
+                R.group_norm_backward(f64(dy), f64(x), groups, f64(mean),
+                                      f64(rstd), f64(gamma), f64(beta), a),
+                what)
+    assert y.dtype == out and dx.dtype == x.dtype
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("shape,groups", [
+    ((1, 1, 1, 1), 1),             # one value: its own mean
+    ((2, 1, 1, 8), 8),             # one value to a group
+    ((3, 5, 7, 24), 4), ((1, 16, 16, 320), 32),   # vectors straddle groups
+    ((2, 9, 1, 33), 3), ((2, 1, 31, 35), 5),      # odd channels
+    ((1, 40, 50, 64), 1), ((2, 33, 17, 66), 2),
+    ((4, 3, 3, 2056), 1),          # a group wider than a block
+    ((1, 6, 5, 4104), 2), ((1, 130, 129, 16), 4)])
+def test_norm_shapes(pair, shape, groups):
+    say(f"[gpu] group norm {shape} / {groups} {pair}")
+    c = shape[-1]
+    x = rnd(1, *shape, dtype=pair[0], shift=0.7)
+    for a in (R.NONE, R.RELU, R.SILU):
+        norm_both(x, groups, rnd(2, c, shift=1.0), rnd(3, c), a, pair[1],
+                  what=f"{shape} {a}")
+    norm_both(x, groups, None, None, R.SILU, pair[1], what="no parameters")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_norm_strides(dtype):
+    """Crops, channel slices at odd offsets, permuted images: read in place;
+    and written into a slice, whose surroundings stay."""
+    say(f"[gpu] group norm strides {dtype}")
+    big = rnd(4, 3, 12, 14, 40, dtype=dtype)
+    for x in (big[:, 1:-1, 2:-1, 8:32], big[..., 1:25], big[:, ::2, ::3, 3:9],
+              big.transpose(1, 2)[..., :24], big.flip(0)[::2][..., :6],
+              big[1:2, :, 5:6, 16:40], big[:, 3:4, :, :8]):
+        norm_both(x, 2, None, None, R.SILU, dtype, what=str(x.stride()))
+    wide = torch.full((3, 12, 14, 40), 7.0, dtype=dtype, device="cuda")
+    x = big[..., :24].contiguous()
+    y, _, _ = ops.group_norm(x, 4, act=1, out=wide[..., 9:33])
+    check(y, *R.group_norm(f64(x), 4, None, None, R.RELU, 1e-5)["y"], "slice")
+    assert (wide[..., :9] == 7).all() and (wide[..., 33:] == 7).all()
+
+
+def test_norm_sites_and_images():
+    """[n, sites, c], no image at all, and many small images."""
+    say("[gpu] group norm, sites and images")
+    norm_both(rnd(5, 2, 77, 12), 3, rnd(6, 12), None, R.SILU, F32, what="3d")
+    norm_both(rnd(7, 700, 2, 2, 8, dtype=BF16), 2, None, rnd(8, 8), R.SILU,
+              BF16, what="many images")
+    x = torch.empty(0, 4, 4, 8, device="cuda")
+    y, m, r = ops.group_norm(x, 2)
+    assert y.shape == x.shape and m.shape == (0, 2)
+    _, dg, db = ops.group_norm_backward(y, x, 2, m, r)
+    assert (dg == 0).all() and (db == 0).all() and dg.shape == (8,)
+
+
+def test_norm_far_mean():
+    """A mean 3000 deviations from zero: nothing cancels (a sum of squares
+    would lose every digit)."""
+    say("[gpu] group norm, far mean")
+    for shape in ((2, 64, 64, 16), (1, 5, 5, 24)):
+        x = rnd(9, *shape, shift=3000.0)
+        norm_both(x, 4, None, None, R.NONE, F32, what="far mean")
+
+
+def test_norm_in_place():
+    say("[gpu] group norm in place")
+    for shape, dtype in (((2, 30, 31, 48), BF16), ((1, 200, 300, 32), F32)):
+        x = rnd(10, *shape, dtype=dtype)
+        want, m, r = ops.group_norm(x, 4, act=2)
+        z = x.clone()
+        got = ops.group_norm(z, 4, act=2, out=z)[0]
+        assert got.data_ptr() == z.data_ptr() and torch.equal(got, want)
+        dy = rnd(11, *shape, dtype=dtype)
+        want = ops.group_norm_backward(dy, x, 4, m, r, act=2)
+        for on in (x.clone(), dy.clone()):
+            args = (dy, on) if on.data_ptr() and torch.equal(on, x) else \
+                (on, x)
+            got = ops.group_norm_backward(*args, 4, m, r, act=2, out=on)
+            for p, q in zip(got, want):
+                assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_norm_relu_kink(dtype):
+    """Quarters throughout, mean and rstd given: z is exact, and zero passes
+    nothing on."""
+    say(f"[gpu] group norm, relu kink {dtype}")
+    x = (rnd(12, 2, 9, 9, 16) * 4).round().to(dtype) / 4
+    mean = torch.full((2, 4), 0.25, device="cuda")
+    rstd = torch.full((2, 4), 0.5, device="cuda")
+    beta = (rnd(13, 16) * 2).round() / 8
+    dy = (rnd(14, 2, 9, 9, 16) * 4).round().to(dtype)
+    got = ops.group_norm_backward(dy, x, 4, mean, rstd, None, beta, act=1)
+    want = R.group_norm_backward(f64(dy), f64(x), 4, f64(mean), f64(rstd),
+                                 None, f64(beta), R.RELU)
+    z = (f64(x) - 0.25) * 0.5 + f64(beta)
+    assert (z == 0).any()
+    compare(dict(zip(("dx", "dgamma", "dbeta"), got)), want, "kink")
+
+
+def test_norm_not_finite():
+    """NaN and infinity spoil their own group and image only."""
+    say("[gpu] group norm, not finite")
+    x = rnd(15, 3, 6, 6, 16)
+    good = ops.group_norm(x, 4)[0]
+    x[1, 2, 3, 5] = float("nan")
+    x[2, 0, 0, 15] = float("inf")
+    y = ops.group_norm(x, 4)[0]
+    assert torch.equal(y[0], good[0])
+    assert torch.isnan(y[1, ..., 4:8]).all() and torch.equal(
+        y[1, ..., :4], good[1, ..., :4]) and torch.equal(
+        y[1, ..., 8:], good[1, ..., 8:])
+    assert not torch.isfinite(y[2, ..., 12:]).any()
+    assert torch.equal(y[2, ..., :12], good[2, ..., :12])
+
+
+# --------------------------------------------------------------- sequences
+
+def axes(kind, t, b, seed=20):
+    g = np.random.default_rng(seed)
+    ln = rs = None
+    if "l" in kind:
+        ln = g.integers(0, t + 1, b).astype(np.int32)
+        ln[0] = t
+        if b > 1:
+            ln[1] = 0
+        if b > 2:
+            ln[2] = t + 5      # counts as t
+    if "r" in kind:
+        rs = (g.random((t, b)) < 0.2).astype(np.uint8) * 3
+    return ln, rs, "b" in kind
+
+
+def dev(a):
+    return None if a is None else torch.from_numpy(a).cuda()
+
+
+KINDS = ["", "l", "r", "b", "lrb"]
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("t,b,c", [(1, 3, 8), (2, 1, 1), (9, 5, 24),
+                                   (40, 4, 37), (67, 3, 130)])
+def test_conv(pair, kind, t, b, c):
+    say(f"[gpu] time conv {t} {b} {c} {kind!r} {pair}")
+    ln, rs, rev = axes(kind, t, b)
+    kw = dict(lengths=dev(ln), reset=dev(rs), reverse=rev)
+    ref = dict(lengths=ln, reset=rs, reverse=rev)
+    x = rnd(21, t, b, c, dtype=pair[0])
+    for k, a, win in ((4, R.SILU, True), (1, R.NONE, False),
+                      (8, R.SILU, False), (3, R.NONE, True), (2, R.RELU, 1)):
+        w, bias = rnd(22, k, c), rnd(23, c) if k != 3 else None
+        wi = rnd(24, k - 1, b, c, dtype=pair[0]) if win else None
+        y, wo = ops.time_conv(x, w, bias, act=a, window=wi,
+                              out_dtype=pair[1], **kw)
+        compare(dict(y=y, window=wo),
+                R.time_conv(f64(x), f64(w), f64(bias), a, f64(wi), **ref),
+                f"k {k}")
+        if a == R.RELU:
+            continue
+        dy = rnd(25, t, b, c, dtype=pair[1])
+        dwo = rnd(26, k - 1, b, c, dtype=pair[0]) if win else None
+        got = ops.time_conv_backward(dy, x, w, bias, act=a, window=wi,
+                                     dwindow_out=dwo, **kw)
+        compare(dict(zip(("dx", "dweight", "dbias", "dwindow"), got)),
+                R.time_conv_backward(f64(dy), f64(x), f64(w), f64(bias), a,
+                                     f64(wi), dwindow_out=f64(dwo), **ref),
+                f"k {k}")
+
+
+@pytest.mark.parametrize("k", range(1, 9))
+def test_conv_taps(k):
+    """Every tap count, on more rows and steps than one block takes."""
+    say(f"[gpu] time conv, {k} taps")
+    t, b, c = 150, 70, 20
+    ln, rs, _ = axes("lr", t, b)
+    x, w = rnd(31, t, b, c), rnd(32, k, c)
+    wi, dy = rnd(33, k - 1, b, c), rnd(34, t, b, c)
+    kw, ref = (dict(lengths=dev(ln), reset=dev(rs)),
+               dict(lengths=ln, reset=rs))
+    y, wo = ops.time_conv(x, w, None, act=2, window=wi, **kw)
+    compare(dict(y=y, window=wo),
+            R.time_conv(f64(x), f64(w), None, R.SILU, f64(wi), **ref), "")
+    got = ops.time_conv_backward(dy, x, w, None, act=2, window=wi, **kw)
+    compare(dict(zip(("dx", "dweight", "dbias", "dwindow"), got)),
+            R.time_conv_backward(f64(dy), f64(x), f64(w), None, R.SILU,
+                                 f64(wi), **ref), "")
+
+
+def test_conv_relu_kink():
+    """Quarters: z is exact, and zero passes nothing on."""
+    say("[gpu] time conv, relu kink")
+    x = (rnd(35, 30, 4, 8) * 4).round() / 4
+    w = (rnd(36, 3, 8) * 2).round() / 2
+    dy = (rnd(37, 30, 4, 8) * 4).round()
+    got = ops.time_conv_backward(dy, x, w, None, act=1)
+    want = R.time_conv_backward(f64(dy), f64(x), f64(w), None, R.RELU)
+    assert (R.time_conv(f64(x), f64(w), None, R.NONE)["y"][0] == 0).any()
+    compare(dict(zip(("dx", "dweight", "dbias"), got)), want, "kink")
+
+
+def scan_both(v, f, o, h, out, kind, what, dh=None):
+    t, b, c = v.shape
+    ln, rs, rev = axes(kind, t, b)
+    kw = dict(lengths=dev(ln), reset=dev(rs), reverse=rev)
+    ref = dict(lengths=ln, reset=rs, reverse=rev)
+    y, ho, st = ops.gated_scan(v, f, o, h=h, out_dtype=out, save=True, **kw)
+    want = R.gated_scan(f64(v), f64(f), f64(o), f64(h), **ref)
+    # kept states behind a row's length are not written
+    known = ~np.isnan(want["states"][0])
+    wv, wb = want.pop("states")
+    check(st[torch.from_numpy(known).cuda()], wv[known], wb[known],
+          f"{what}: states")
+    compare(dict(y=y, h=ho), want, what)
+    y2, ho2 = ops.gated_scan(v, f, o, h=h, out_dtype=out, **kw)
+    assert torch.equal(y, y2) and torch.equal(ho, ho2)
+    dy = rnd(47, t, b, c, dtype=out)
+    got = ops.gated_scan_backward(dy, v, f, o, states=st, dh=dh, **kw)
+    want = R.gated_scan_backward(f64(dy), f64(v), f64(f), f64(o), f64(h),
+                                 dh=f64(dh), **ref)
+    if o is None:
+        want.pop("do")
+    compare(dict(zip(("dv", "df", "do", "dh"), got)), want, what)
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("t,b,c", [(1, 3, 8), (2, 1, 1), (9, 5, 24),
+                                   (33, 4, 37), (130, 3, 66), (600, 3, 8)])
+def test_scan(pair, kind, t, b, c):
+    say(f"[gpu] gated scan {t} {b} {c} {kind!r} {pair}")
+    v, o = rnd(41, t, b, c, dtype=pair[0]), rnd(42, t, b, c, dtype=pair[0])
+    f = rnd(43, t, b, c, dtype=pair[0], scale=3.0, shift=2.0)
+    h, dh = rnd(44, b, c), rnd(45, b, c)
+    scan_both(v, f, o, h, pair[1], kind, "gate", dh)
+    scan_both(v, f, None, None, pair[1], kind, "plain")
+
+
+@pytest.mark.parametrize("t,b,c,kind", [
+    (5000, 1, 64, ""), (4099, 2, 40, "lr"), (20011, 1, 3, "b"),
+    (33001, 1, 2, "")])
+def test_scan_long(t, b, c, kind):
+    """Long rows, gates that hold for thousands of steps among them."""
+    say(f"[gpu] gated scan, long {t}")
+    v, o = rnd(51, t, b, c, dtype=BF16), rnd(52, t, b, c, dtype=BF16)
+    f = rnd(53, t, b, c, dtype=BF16, scale=1.0, shift=5.0)
+    f[:, :, : c // 2] += 4
+    scan_both(v, f, o, rnd(54, b, c), BF16, kind, "long", rnd(55, b, c))
+
+
+def test_scan_wide():
+    say("[gpu] gated scan, wide")
+    for t, b, c in ((17, 400, 96), (9, 64, 515)):
+        v, f = rnd(56, t, b, c), rnd(57, t, b, c, shift=1.0)
+        scan_both(v, f, rnd(58, t, b, c), rnd(59, b, c), F32, "lr", "wide")
+
+
+def test_scan_gates_at_their_ends():
+    """Gates at infinity: the state is kept to the bit, or replaced; large
+    finite gates let the last digits through."""
+    say("[gpu] gated scan, gates at their ends")
+    t, b, c = 40, 2, 8
+    v, h = rnd(60, t, b, c), rnd(61, b, c)
+    f = torch.full((t, b, c), float("inf"), device="cuda")
+    y, ho = ops.gated_scan(v, f, h=h)
+    assert torch.equal(ho, h) and (y == h).all()
+    y, ho = ops.gated_scan(v, -f, h=h)
+    assert torch.equal(y, v) and torch.equal(ho, v[-1])
+    f = torch.full((t, b, c), 30.0, device="cuda")
+    one = torch.ones(t, b, c, device="cuda") * 1e6
+    y, _ = ops.gated_scan(one, f)
+    want = R.gated_scan(f64(one), f64(f), None)["y"]
+    check(y, *want, "large gates")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_sequence_strides(dtype):
+    """Slices of one wide tensor (aligned and not), rows before time, steps
+    apart; gradients written into slices of one tensor, the rest of which
+    stays."""
+    say(f"[gpu] sequence strides {dtype}")
+    t, b = 21, 5
+    for c, wide in ((16, 48), (10, 33), (7, 24)):
+        z = rnd(62, t, b, wide, dtype=dtype)
+        v, f, o = z[..., :c], z[..., c:2 * c], z[..., 2 * c:3 * c]
+        scan_both(v, f, o, None, dtype, "", f"slices of {c}")
+        scan_both(v[::2], f[::2], o[::2], None, dtype, "l", "steps apart")
+        zt = rnd(63, b, t, wide, dtype=dtype).transpose(0, 1)
+        scan_both(zt[..., :c], zt[..., c:2 * c], zt[..., 2 * c:3 * c], None,
+                  dtype, "b", "rows first")
+        w = rnd(64, 4, c)
+        for x in (v, f, zt[..., 1:1 + c]):
+            y, _ = ops.time_conv(x, w, act=2)
+            check(y, *R.time_conv(f64(x), f64(w), None, R.SILU)["y"],
+                  "conv of a slice")
+        y, _, st = ops.gated_scan(v, f, o, save=True)
+        want = ops.gated_scan_backward(y, v, f, o, states=st)
+        g = torch.full((t, b, wide + 2), 5.0, dtype=dtype, device="cuda")
+        got = ops.gated_scan_backward(
+            y, v, f, o, states=st,
+            out=(g[..., :c], g[..., c:2 * c], g[..., 2 * c:3 * c]))
+        for p, q in zip(got, want):
+            assert torch.equal(p, q)
+        assert (g[..., 3 * c:] == 5).all()
+
+
+def test_sequence_shared_inputs():
+    """Broadcast rows and one tensor for two inputs are read as they are."""
+    say("[gpu] sequences, shared inputs")
+    x = rnd(65, 12, 1, 16)
+    v = x.expand(12, 4, 16)
+    scan_both(v, v, v, None, F32, "l", "one tensor for all")
+    w = rnd(66, 3, 16)
+    y, _ = ops.time_conv(v, w)
+    check(y, *R.time_conv(f64(v), f64(w), None, R.NONE)["y"], "expanded")
+
+
+def test_sequence_empty():
+    say("[gpu] sequences without steps or rows")
+    h, win = rnd(67, 3, 8), rnd(68, 2, 3, 8)
+    x = torch.empty(0, 3, 8, device="cuda")
+    y, ho, st = ops.gated_scan(x, x, x, h=h, save=True)
+    assert torch.equal(ho, h) and st.shape == (0, 3, 8)
+    *_, dh = ops.gated_scan_backward(y, x, x, x, states=st, dh=h)
+    assert torch.equal(dh, h)
+    assert (ops.gated_scan(x, x)[1] == 0).all()
+    w = rnd(69, 3, 8)
+    y, wo = ops.time_conv(x, w, window=win)
+    assert torch.equal(wo, win)
+    dx, dw, db, dwin = ops.time_conv_backward(y, x, w, window=win,
+                                              dwindow_out=win)
+    assert (dw == 0).all() and (db == 0).all() and torch.equal(dwin, win)
+    x = torch.empty(4, 0, 8, device="cuda")
+    assert ops.gated_scan(x, x)[0].shape == x.shape
+    _, dw, db, _ = ops.time_conv_backward(x, x, w)
+    assert (dw == 0).all() and (db == 0).all()
+    # all rows empty: zeros, and the state stays
+    x = rnd(70, 6, 3, 8)
+    ln = torch.zeros(3, dtype=torch.int32, device="cuda")
+    y, ho = ops.gated_scan(x, x, h=h, lengths=ln)
+    assert (y == 0).all() and torch.equal(ho, h)
+    y, wo = ops.time_conv(x, w, act=2, bias=w[0], window=win, lengths=ln)
+    assert (y == 0).all() and torch.equal(wo, win)
+
+
+def test_padding_is_not_read():
+    """What lies behind a row's length, NaN here, reaches nothing."""
+    say("[gpu] padding is not read")
+    t, b, c = 50, 4, 12
+    ln = torch.tensor([50, 0, 17, 33], dtype=torch.int32, device="cuda")
+    live = torch.arange(t, device="cuda")[:, None] < ln[None]
+    x, f = rnd(71, t, b, c), rnd(72, t, b, c)
+    w, dy = rnd(73, 4, c), rnd(74, t, b, c)
+    nan = [torch.where(live[..., None], q, float("nan")) for q in (x, f, dy)]
+    for rev in (False, True):
+        kw = dict(lengths=ln, reverse=rev)
+        res = []
+        for p, q, d in ((x, f, dy), nan):
+            y, h, st = ops.gated_scan(p, q, p, save=True, **kw)
+            st = torch.where(torch.arange(0, t, 16, device="cuda")[
+                :, None, None] < ln[None, :, None], st, 0.0)
+            z, win = ops.time_conv(p, w, act=2, **kw)
+            res.append([y, h, z, win,
+                        *ops.gated_scan_backward(d, p, q, p, states=st, **kw),
+                        *ops.time_conv_backward(d, p, w, act=2, **kw)])
+        for p, q in zip(*res):
+            assert torch.equal(p, q) and torch.isfinite(p).all()
+
+
+# ------------------------------------------------------- steps and chunks
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_steps_equal_the_chunk(dtype):
+    """Single steps with the window and the state kept in place give the
+    chunk's outputs to the bit, however the chunk is cut."""
+    say(f"[gpu] steps and chunk {dtype}")
+    t, b, c, k = 23, 6, 40, 4
+    x, f, o = (rnd(80 + i, t, b, c, dtype=dtype) for i in range(3))
+    w, win0, h0 = rnd(83, k, c), rnd(84, k - 1, b, c, dtype=dtype), rnd(85, b,
+                                                                        c)
+    win, h = win0.clone(), h0.clone()
+    u, wo = ops.time_conv(x, w, act=2, window=win)
+    y, ho = ops.gated_scan(u, f, o, h=h)
+    cuts = [0, 1, 2, 3, 9, 10, 17, 23]
+    us, ys = [], []
+    for s, e in zip(cuts, cuts[1:]):
+        q, _ = ops.time_conv(x[s:e], w, act=2, window=win, window_out=win)
+        r, _ = ops.gated_scan(q, f[s:e], o[s:e], h=h, h_out=h)
+        us.append(q)
+        ys.append(r)
+    assert torch.equal(torch.cat(us), u) and torch.equal(win, wo)
+    assert torch.equal(torch.cat(ys), y) and torch.equal(h, ho)
+
+
+def test_gradients_through_chunks():
+    """A row cut in two, the gradients of state and window handed back,
+    equals the whole row."""
+    say("[gpu] gradients through chunks")
+    t, b, c, k, m = 40, 3, 16, 4, 19
+    x, f, o, dy = (rnd(90 + i, t, b, c) for i in range(4))
+    w = rnd(95, k, c)
+    y, h, st = ops.gated_scan(x, f, o, save=True)
+    whole = ops.gated_scan_backward(dy, x, f, o, states=st)
+    _, h1, s1 = ops.gated_scan(x[:m], f[:m], o[:m], save=True)
+    _, h2, s2 = ops.gated_scan(x[m:], f[m:], o[m:], h=h1, save=True)
+    g2 = ops.gated_scan_backward(dy[m:], x[m:], f[m:], o[m:], states=s2)
+    g1 = ops.gated_scan_backward(dy[:m], x[:m], f[:m], o[:m], states=s1,
+                                 dh=g2[3])
+    want = R.gated_scan_backward(f64(dy), f64(x), f64(f), f64(o))
+    for i, n in enumerate(("dv", "df", "do")):
+        check(torch.cat([g1[i], g2[i]]), *want[n], n)
+        check(whole[i], *want[n], n)
+    win = x[m - 3:m].contiguous()
+    d2 = ops.time_conv_backward(dy[m:], x[m:], w, act=2, window=win)
+    d1 = ops.time_conv_backward(dy[:m], x[:m], w, act=2, dwindow_out=d2[3])
+    want = R.time_conv_backward(f64(dy), f64(x), f64(w), None, R.SILU)
+    check(torch.cat([d1[0], d2[0]]), want["dx"][0],
+          want["dx"][1] + 2.0 ** -23 * np.abs(want["dx"][0]), "dx")
+
+
+# ---------------------------------------------------- streams, graphs, runs
+
+def everything(x3, x4, w):
+    y, m, r = ops.group_norm(x4, 4, act=2)
+    u, win = ops.time_conv(x3, w, act=2)
+    z, h, st = ops.gated_scan(u, x3, x3, save=True)
+    return [y, m, r, u, win, z, h,
+            *ops.group_norm_backward(y, x4, 4, m, r, act=2),
+            *ops.time_conv_backward(z, x3, w, act=2),
+            *ops.gated_scan_backward(z, u, x3, x3, states=st)]
+
+
+def test_repeats_streams_and_graphs():
+    """The same bits from run to run, on another stream, from two streams at
+    once, and from a captured graph replayed over other inputs and between
+    eager calls."""
+    say("[gpu] repeats, streams, graphs")
+    mk = [(rnd(100 + i, 700, 3, 40, dtype=BF16),
+           rnd(110 + i, 2, 50, 60, 48, dtype=BF16), rnd(120 + i, 4, 40))
+          for i in range(3)]
+    want = [everything(*m) for m in mk]
+    for a, b in zip(everything(*mk[0]), want[0]):
+        assert torch.equal(a, b)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = everything(*mk[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for a, b in zip(got[i], want[i]):
+            assert torch.equal(a, b)
+    slot = [q.clone() for q in mk[0]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = everything(*slot)
+    for i in (0, 1, 2, 1, 0):
+        for s, q in zip(slot, mk[i]):
+            s.copy_(q)
+        graph.replay()
+        for a, b in zip(res, want[i]):
+            assert torch.equal(a, b)
+        everything(*mk[(i + 1) % 3])
+        torch.cuda.synchronize()
+
+
+def test_tensor_refusals():
+    say("[gpu] refusals of tensors")
+    x = rnd(130, 4, 3, 8)
+    x4 = rnd(131, 2, 3, 3, 8)
+    w, i32 = rnd(132, 3, 8), torch.zeros(3, dtype=torch.int32, device="cuda")
+    from paper_2410_20790_amd import StError
+    for err, fn in (
+            (ValueError, lambda: ops.group_norm(x4.double(), 2)),
+            (ValueError, lambda: ops.group_norm(x4.movedim(-1, 1), 3)),
+            (ValueError, lambda: ops.group_norm(x4[0, 0], 2)),
+            (ValueError, lambda: ops.group_norm(x4, 2, w[0].half())),
+            (ValueError, lambda: ops.group_norm(x4, 2, w[0, :4])),
+            (ValueError, lambda: ops.group_norm(x4.half(), 2,
+                                                out_dtype=F32)),
+            (ValueError, lambda: ops.group_norm(x4, 2, out=x4[:1])),
+            (StError, lambda: ops.group_norm(x4, 3)),
+            (StError, lambda: ops.group_norm(x4[:1], 2,
+                                             out=x4[:1].expand(1, 3, 3, 8)
+                                             [:, :, :1].expand(1, 3, 3, 8))),
+            (ValueError, lambda: ops.group_norm_backward(
+                x4.half(), x4, 2, w[:2, :2], w[:2, :2])),
+            (ValueError, lambda: ops.time_conv(x, rnd(1, 9, 8))),
+            (ValueError, lambda: ops.time_conv(x, w.t())),
+            (ValueError, lambda: ops.time_conv(x, w, window=x[:2].half())),
+            (ValueError, lambda: ops.time_conv(x, w, lengths=i32.long())),
+            (ValueError, lambda: ops.time_conv(x, w, lengths=i32[:2])),
+            (ValueError, lambda: ops.time_conv(x, w, reset=i32)),
+            (StError, lambda: ops.time_conv(x, w, out=x)),
+            (ValueError, lambda: ops.gated_scan(x, x.half())),
+            (ValueError, lambda: ops.gated_scan(x, x[:, :2])),
+            (ValueError, lambda: ops.gated_scan(x, x, h=x[0].half())),
+            (ValueError, lambda: ops.gated_scan(x, x, h=x[0].cpu())),
+            (StError, lambda: ops.gated_scan(x, x, out=x)),
+            (ValueError, lambda: ops.gated_scan_backward(
+                x, x, x, states=x)),
+            (ValueError, lambda: ops.gated_scan_backward(
+                x, x, x, x, states=ops.kept_states(4, 3, 8, "cuda"),
+                out=(x.clone(), x.clone())))):
+        with pytest.raises(err):
+            fn()
