@@ -348,6 +348,40 @@ def test_sequence_strides(dtype):
         assert (g[..., 3 * c:] == 5).all()
 
 
+def test_reset_stops_what_is_not_finite():
+    """NaN and infinity before a reset do not pass it, in short rows and in
+    rows split along time; nor do they reach back over it."""
+    say("[gpu] resets and what is not finite")
+    for t, at, spoil in ((20, 9, 4), (700, 300, 250), (9000, 4500, 20)):
+        v, f = rnd(140, t, 2, 8), rnd(141, t, 2, 8, shift=2.0)
+        dy = rnd(142, t, 2, 8)
+        reset = torch.zeros(t, 2, dtype=torch.uint8, device="cuda")
+        reset[at] = 1
+        y, h, st = ops.gated_scan(v, f, v, reset=reset, save=True)
+        g = ops.gated_scan_backward(dy, v, f, v, states=st, reset=reset)
+        for bad in (float("nan"), float("inf")):
+            v2, dy2 = v.clone(), dy.clone()
+            v2[spoil, 0, 3] = bad
+            y2, h2, s2 = ops.gated_scan(v2, f, v, reset=reset, save=True)
+            assert torch.equal(y2[at:], y[at:]) and torch.equal(h2, h)
+            assert not torch.isfinite(y2[at - 1, 0, 3])
+            keep = torch.ones_like(y2, dtype=torch.bool)
+            keep[spoil:at, 0, 3] = False
+            assert torch.equal(y2[keep], y[keep])
+            dy2[t - 1, 1, 2] = bad
+            g2 = ops.gated_scan_backward(dy2, v, f, v, states=st,
+                                         reset=reset)
+            for p, q in zip(g2[:3], g):
+                assert torch.equal(p[:at], q[:at])
+                assert not torch.isfinite(p[t - 1, 1, 2])
+        x2 = v.clone()
+        x2[at - 1] = float("nan")
+        w = rnd(143, 4, 8)
+        p = ops.time_conv(v, w, reset=reset)[0]
+        q = ops.time_conv(x2, w, reset=reset)[0]
+        assert torch.equal(p[at:], q[at:]) and torch.isnan(q[at - 1]).all()
+
+
 def test_sequence_shared_inputs():
     """Broadcast rows and one tensor for two inputs are read as they are."""
     say("[gpu] sequences, shared inputs")
