@@ -28,9 +28,10 @@ struct ScanArgs {
   int64_t lanes;                   // b * cv
   // rows split along time
   int cols;                        // blocks of 64 lanes
-  int tiles, subs;                 // tiles of a row, rounds of a tile
-  float* ends;                     // [tiles]{A, H}, then the state: [b][c]
+  int tiles, group;                // tiles of a row, tiles of a group
+  void* ends;                      // the ticket, then words: tiles, groups
 };
+constexpr int kHeadWords = 2;
 
 template <typename T, typename O, int V, bool GATE>
 __global__ __launch_bounds__(kThreads) void k_scan(ScanArgs a) {
@@ -92,275 +93,6 @@ __global__ __launch_bounds__(kThreads) void k_scan(ScanArgs a) {
   if (a.h_out) {
 #pragma unroll
     for (int e = 0; e < V; ++e) a.h_out[hc + e] = h[e];
-  }
-}
-
-// ------------------------------------------------- rows split along time
-//
-// Few rows and channels, many steps: a thread for each would leave the device
-// idle.  h_s = a_s h_{s-1} + u_s joins: a run of steps acts as h -> A h + H
-// with A the product of its a.  A block takes 64 lanes (a lane: V adjacent
-// channels of a row) over W waves, a wave kSplit steps of each lane, whose
-// inputs stay in its registers: the waves exchange their (A, H) through LDS,
-// fold those before them in order, and then run their steps from the state
-// that enters them.  A tile is `subs` such rounds.  Where a row has several
-// tiles a first launch leaves every tile's (A, H); the second folds those
-// before it.  All folds run in step order: the same bits in every run.
-
-constexpr int kSplit = 16;       // steps of a wave
-constexpr int kWaves = 8;        // waves of a block, along time
-constexpr int kRound = kSplit * kWaves;
-static_assert(kSplit == kStride, "a wave keeps the state before its steps");
-
-// A reset is a factor of minus zero (gates are never negative), which no value
-// passes, not even NaN.
-__device__ __forceinline__ bool is_cut(float A) {
-  return __float_as_uint(A) == 0x80000000u;
-}
-
-// The time of step s, or of the row's nearest (time 0 of a row of none).
-__device__ __forceinline__ int64_t time_in(const Row& r, int s) {
-  const int64_t t = time_of(r, max(0, min(s, r.len - 1)));
-  return t < 0 ? 0 : t;
-}
-
-struct LaneAt {
-  int b, ch;
-  bool on;          // otherwise a copy of the last lane that stores nothing
-  int64_t hc;
-};
-__device__ __forceinline__ LaneAt lane_at(const ScanArgs& a, int v) {
-  int64_t lane = (int64_t)(blockIdx.x % a.cols) * 64 + (threadIdx.x & 63);
-  LaneAt l;
-  l.on = lane < a.lanes;
-  if (!l.on) lane = a.lanes - 1;
-  l.b = (int)(lane / a.cv);
-  l.ch = (int)(lane % a.cv) * v;
-  l.hc = (int64_t)l.b * a.q.c + l.ch;
-  return l;
-}
-
-// Folds `n` entries of (A, H), `step` floats apart, into (A, H) in order.
-template <int V>
-__device__ __forceinline__ void fold(const float* pa, const float* ph, int n,
-                                     int64_t step, float* A, float* H) {
-  for (int i = 0; i < n; ++i) {
-    float x[V], y[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      x[e] = pa[i * step + e];
-      y[e] = ph[i * step + e];
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const bool cut = is_cut(x[e]);
-      H[e] = cut ? y[e] : __builtin_fmaf(x[e], H[e], y[e]);
-      A[e] = cut ? x[e] : A[e] * x[e];
-    }
-  }
-}
-
-// The (A, H) of a wave's steps [s0, s0 + kSplit).
-template <typename T, int V>
-__device__ __forceinline__ void wave_ends(const ScanArgs& a, const Row& r,
-                                          int b, int s0,
-                                          const Pack<T, V>* iv,
-                                          const Pack<T, V>* jf, float* A,
-                                          float* H) {
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    A[e] = 1.f;
-    H[e] = 0.f;
-  }
-#pragma unroll
-  for (int k = 0; k < kSplit; ++k) {
-    float v[V], f[V];
-    unpack<T, V>(iv[k], v);
-    unpack<T, V>(jf[k], f);
-    const bool live = s0 + k < r.len;
-    const bool cut = live && reset_at(a.q, r, b, s0 + k);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float keep, write;
-      sigmoids(f[e], keep, write);
-      const float h = __builtin_fmaf(keep, cut ? 0.f : H[e], write * v[e]);
-      H[e] = live ? h : H[e];
-      A[e] = live ? (cut ? -0.f : A[e] * keep) : A[e];
-    }
-  }
-}
-
-template <typename T, int V>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_ends(ScanArgs a) {
-  __shared__ float sa[kWaves][64 * V], sh[kWaves][64 * V];
-  const int wave = threadIdx.x / 64, at = (threadIdx.x & 63) * V;
-  const int tile = blockIdx.x / a.cols;
-  const LaneAt l = lane_at(a, V);
-  const Row r = row_of(a.q, l.b);
-  const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
-  const T* pf = (const T*)a.f.p + (int64_t)l.b * a.f.sb + l.ch;
-  float TA[V], TH[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    TA[e] = 1.f;
-    TH[e] = 0.f;
-  }
-  for (int sub = 0; sub < a.subs; ++sub) {
-    const int s0 = (tile * a.subs + sub) * kRound + wave * kSplit;
-    float A[V], H[V];
-    if (__any(s0 < r.len)) {
-      Pack<T, V> iv[kSplit], jf[kSplit];
-#pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        const int64_t tc = time_in(r, s0 + k);
-        iv[k] = load_pack<T, V>(pv + tc * a.v.st);
-        jf[k] = load_pack<T, V>(pf + tc * a.f.st);
-      }
-      wave_ends<T, V>(a, r, l.b, s0, iv, jf, A, H);
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        A[e] = 1.f;
-        H[e] = 0.f;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = H[e];
-    }
-    __syncthreads();
-    if (wave == 0) fold<V>(&sa[0][at], &sh[0][at], kWaves, 64 * V, TA, TH);
-  }
-  if (wave == 0 && l.on) {
-    const int64_t plane = (int64_t)a.q.b * a.q.c;
-    float* o = a.ends + (int64_t)tile * 2 * plane + l.hc;
-    store_pack<float, V>(o, TA);
-    store_pack<float, V>(o + plane, TH);
-    // the state itself too: the second launch may replace it in place
-    if (tile == 0) {
-      float h[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = a.h ? a.h[l.hc + e] : 0.f;
-      store_pack<float, V>(a.ends + (int64_t)a.tiles * 2 * plane + l.hc, h);
-    }
-  }
-}
-
-template <typename T, typename O, int V, bool GATE>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_tiles(ScanArgs a) {
-  __shared__ float sa[kWaves][64 * V], sh[kWaves][64 * V];
-  const int wave = threadIdx.x / 64, at = (threadIdx.x & 63) * V;
-  const int tile = blockIdx.x / a.cols;
-  const LaneAt l = lane_at(a, V);
-  const Row r = row_of(a.q, l.b);
-  const int64_t plane = (int64_t)a.q.b * a.q.c;
-  const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
-  const T* pf = (const T*)a.f.p + (int64_t)l.b * a.f.sb + l.ch;
-  const T* po =
-      GATE ? (const T*)a.o.p + (int64_t)l.b * a.o.sb + l.ch : nullptr;
-  O* py = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
-  // the state that enters the tile: waves fold shares of the tiles before it
-  float h[V];
-  if (a.tiles == 1) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = a.h ? a.h[l.hc + e] : 0.f;
-  } else {
-    float A[V], H[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = 1.f;
-      H[e] = 0.f;
-      h[e] = a.ends[(int64_t)a.tiles * 2 * plane + l.hc + e];
-    }
-    const int share = (tile + kWaves - 1) / kWaves;
-    const int i0 = min(wave * share, tile), i1 = min(i0 + share, tile);
-    const float* e0 = a.ends + (int64_t)i0 * 2 * plane + l.hc;
-    fold<V>(e0, e0 + plane, i1 - i0, 2 * plane, A, H);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = H[e];
-    }
-    __syncthreads();
-    fold<V>(&sa[0][at], &sh[0][at], kWaves, 64 * V, A, h);
-  }
-  for (int sub = 0; sub < a.subs; ++sub) {
-    const int s0 = (tile * a.subs + sub) * kRound + wave * kSplit;
-    const bool any = __any(s0 < r.len);
-    Pack<T, V> iv[kSplit], jf[kSplit], io[kSplit];
-    float A[V], H[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = 1.f;
-      H[e] = 0.f;
-    }
-    if (any) {
-#pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        const int64_t tc = time_in(r, s0 + k);
-        iv[k] = load_pack<T, V>(pv + tc * a.v.st);
-        jf[k] = load_pack<T, V>(pf + tc * a.f.st);
-        if (GATE) io[k] = load_pack<T, V>(po + tc * a.o.st);
-      }
-      wave_ends<T, V>(a, r, l.b, s0, iv, jf, A, H);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = H[e];
-    }
-    __syncthreads();
-    float hw[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) hw[e] = h[e];
-    fold<V>(&sa[0][at], &sh[0][at], wave, 64 * V, A, hw);
-    // the round's end: the same sums, carried on to every wave
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = hw[e];
-    fold<V>(&sa[wave][at], &sh[wave][at], kWaves - wave, 64 * V, A, h);
-    if (any && l.on) {
-      if (a.states && s0 < r.len)
-        store_pack<float, V>(a.states + (s0 / kStride) * plane + l.hc, hw);
-#pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        if (s0 + k < r.len) {
-          const bool cut = reset_at(a.q, r, l.b, s0 + k);
-          float v[V], f[V], y[V];
-          unpack<T, V>(iv[k], v);
-          unpack<T, V>(jf[k], f);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float keep, write;
-            sigmoids(f[e], keep, write);
-            hw[e] = __builtin_fmaf(keep, cut ? 0.f : hw[e], write * v[e]);
-            y[e] = hw[e];
-          }
-          if (GATE) {
-            float o[V];
-            unpack<T, V>(io[k], o);
-#pragma unroll
-            for (int e = 0; e < V; ++e) y[e] *= sigmoid(o[e]);
-          }
-          store_pack<O, V>(py + time_of(r, s0 + k) * a.y.st, y);
-        }
-      }
-    }
-    if (l.on) {
-      const int s1 = min(s0 + kSplit, a.q.t);
-      for (int s = max(s0, r.len); s < s1; ++s) {
-        float z[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) z[e] = 0.f;
-        store_pack<O, V>(py + (int64_t)s * a.y.st, z);
-      }
-    }
-  }
-  if (a.h_out && tile == a.tiles - 1 && wave == 0 && l.on) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) a.h_out[l.hc + e] = h[e];
   }
 }
 
@@ -464,108 +196,377 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(ScanArgs a) {
   }
 }
 
-// The backward pass of rows split along time: dh runs from the last step to
-// the first, d -> A d + D over a run of steps, and joins the same way.  The
-// states come again, wave by wave, from those kept.  (The folds go from the
-// last entry down.)
+// ------------------------------------------------- rows split along time
+//
+// Few rows and channels, many steps: a thread for each would leave the device
+// idle.  h_s = a_s h_{s-1} + u_s joins: a run of steps acts as h -> A h + H
+// with A the product of its a (d -> A d + D for the gradient, whose order is
+// the reverse).  A block takes a tile: 64 lanes (V adjacent channels of a row
+// each) over W waves, a wave kSplit steps of every lane.  Gates and inputs of
+// these steps stay in registers, so that all is read once and every gate
+// computed once; the tile's (A, H) is published, those of the tiles before it
+// are folded, and the steps are run from the state that enters.
+//
+// Tiles are numbered by a ticket, so a block only waits for blocks that run
+// already, and these publish before they wait for anything themselves.  The
+// fold is in two levels, groups of `group` tiles and the tiles of the block's
+// own group, both in running order and cut by sizes alone: the same bits in
+// every run.  (Publishing states instead, each from the one before, would be
+// a chain of as many memory round trips as there are tiles; taking whatever
+// is there first would change the order of the roundings.)
+
+constexpr int kSplit = ST_SCAN_STRIDE;   // steps of a wave
+
+// A reset is a factor of minus zero (gates are never negative), which no value
+// passes, not even NaN.
+constexpr float kCut = -0.f;
+__device__ __forceinline__ bool is_cut(float A) {
+  return __float_as_uint(A) == 0x80000000u;
+}
+
+// The time of step s, or of the row's nearest (time 0 of a row of none).
+__device__ __forceinline__ int64_t time_in(const Row& r, int s) {
+  const int64_t t = time_of(r, max(0, min(s, r.len - 1)));
+  return t < 0 ? 0 : t;
+}
+
+// (A, H), then (x, y): the steps of (x, y) run after those of (A, H).
 template <int V>
-__device__ __forceinline__ void fold_back(const float* pa, const float* pd,
-                                          int n, int64_t step, float* A,
-                                          float* D) {
-  fold<V>(pa + (n - 1) * step, pd + (n - 1) * step, n, -step, A, D);
+__device__ __forceinline__ void then(float* A, float* H, const float* x,
+                                     const float* y) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const bool cut = is_cut(x[e]);
+    H[e] = cut ? y[e] : __builtin_fmaf(x[e], H[e], y[e]);
+    A[e] = cut ? x[e] : A[e] * x[e];
+  }
+}
+template <int V>
+__device__ __forceinline__ void none(float* A, float* H) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    A[e] = 1.f;
+    H[e] = 0.f;
+  }
 }
 
-// One step back: dh of the step is d + g; what goes on to the step before.
-__device__ __forceinline__ float back(float d, float keep, bool cut) {
-  return cut ? 0.f : d * keep;
+// A published value: its bits beside a mark, in one 8-byte word, so that it
+// is whole when it is seen.  Words start as zeros.
+typedef unsigned long long Word;
+__device__ __forceinline__ void publish(Word* w, float x) {
+  __hip_atomic_store(w, (1ull << 32) | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Word peek(const Word* w) {
+  return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <typename T, typename O, int V, bool GATE>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_grad_ends(ScanArgs a) {
-  __shared__ float sa[kWaves][64 * V], sh[kWaves][64 * V];
-  const int wave = threadIdx.x / 64, at = (threadIdx.x & 63) * V;
-  const int tile = blockIdx.x / a.cols;
-  const LaneAt l = lane_at(a, V);
+// The places of published (A, H): entry i of this block's lanes.
+struct Ends {
+  Word* base;        // of entry 0, this lane
+  int64_t plane;     // words of an entry's A (its H follows)
+};
+template <int V>
+__device__ __forceinline__ void put_entry(const Ends& p, int64_t i,
+                                          const float* A, const float* H) {
+  Word* w = p.base + i * 2 * p.plane;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    publish(w + e, A[e]);
+    publish(w + p.plane + e, H[e]);
+  }
+}
+// Folds entries [i0, i1) into (A, H), four at a time, waiting for each.
+template <int V>
+__device__ __forceinline__ void fold_entries(const Ends& p, int64_t i0,
+                                             int64_t i1, float* A, float* H) {
+  for (int64_t i = i0; i < i1; i += 4) {
+    Word w[4][2 * V];
+    bool all;
+    do {
+      all = true;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const Word* q = p.base + min(i + k, i1 - 1) * 2 * p.plane;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          w[k][e] = peek(q + e);
+          w[k][V + e] = peek(q + p.plane + e);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) all = all && (w[k][e] >> 32) != 0;
+      if (!all) __builtin_amdgcn_s_sleep(2);
+    } while (!all);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (i + k < i1) {
+        float x[V], y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          x[e] = __uint_as_float((uint32_t)w[k][e]);
+          y[e] = __uint_as_float((uint32_t)w[k][V + e]);
+        }
+        then<V>(A, H, x, y);
+      }
+    }
+  }
+}
+
+// A block's lanes and waves, in running order: wave 0 has the first steps to
+// run (of the backward pass: the row's last).
+template <int V, int W>
+struct TileShared {
+  float a[W][64 * V], h[W][64 * V];
+  int ticket;
+};
+
+// Joins the waves' (A, H) in LDS: each wave gets what runs before it in `A, H`
+// and every wave the whole in `TA, TH`.
+template <int V, int W>
+__device__ __forceinline__ void join_waves(TileShared<V, W>& sh, int wave,
+                                           float* A, float* H, float* TA,
+                                           float* TH) {
+  const int at = (threadIdx.x & 63) * V;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    sh.a[wave][at + e] = A[e];
+    sh.h[wave][at + e] = H[e];
+  }
+  __syncthreads();
+  none<V>(TA, TH);
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w == wave) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        A[e] = TA[e];
+        H[e] = TH[e];
+      }
+    }
+    then<V>(TA, TH, &sh.a[w][at], &sh.h[w][at]);
+  }
+}
+
+// What enters this tile (its k-th in running order): the state `h` after all
+// tiles before it, given the tile's own (TA, TH).  h comes in as the state
+// before the first tile, which only tile 0 has (the row's state may be
+// replaced in place once the last tile has run).
+template <int V, int W>
+__device__ __forceinline__ void enter_tile(const ScanArgs& a,
+                                           TileShared<V, W>& sh, int k,
+                                           int col, int wave, float* TA,
+                                           float* TH, float* h) {
+  if (a.tiles == 1) return;
+  Ends p;
+  p.plane = (int64_t)a.cols * 64 * V;
+  p.base = (Word*)a.ends + kHeadWords +
+           ((int64_t)col * 64 + (threadIdx.x & 63)) * V;
+  if (k == 0) {
+    // nothing enters but h: the tile's end is a state
+    if (wave == 0) {
+      float cut[V], end[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        cut[e] = kCut;
+        end[e] = is_cut(TA[e]) ? TH[e] : __builtin_fmaf(TA[e], h[e], TH[e]);
+      }
+      put_entry<V>(p, 0, cut, end);
+    }
+    return;
+  }
+  if (wave == 0) put_entry<V>(p, k, TA, TH);
+  const int g = k / a.group, in = k % a.group;
+  float A[V], H[V], PA[V], PH[V];
+  // the tiles of its group before it, a share to each wave
+  none<V>(A, H);
+  const int share = (in + W - 1) / W;
+  const int64_t g0 = (int64_t)g * a.group;
+  fold_entries<V>(p, g0 + min(wave * share, in),
+                  g0 + min((wave + 1) * share, in), A, H);
+  join_waves<V, W>(sh, wave, A, H, PA, PH);
+  if (in == a.group - 1 && wave == 0 && k < a.tiles - 1) {
+    // the last of its group publishes the group
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      A[e] = PA[e];
+      H[e] = PH[e];
+    }
+    then<V>(A, H, TA, TH);
+    put_entry<V>(p, (int64_t)a.tiles + g, A, H);
+  }
+  // the groups before its own
+  none<V>(A, H);
+  const int gs = (g + W - 1) / W;
+  fold_entries<V>(p, (int64_t)a.tiles + min(wave * gs, g),
+                  (int64_t)a.tiles + min((wave + 1) * gs, g), A, H);
+  float GA[V], GH[V];
+  join_waves<V, W>(sh, wave, A, H, GA, GH);
+  then<V>(GA, GH, PA, PH);
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = GH[e];
+}
+
+// Clears the words and the ticket of a launch.
+__global__ __launch_bounds__(256) void k_scan_clear(uint4* w, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * 256)
+    w[i] = make_uint4(0, 0, 0, 0);
+}
+
+struct LaneAt {
+  int b, ch;
+  bool on;          // otherwise a copy of the last lane that stores nothing
+  int64_t hc;
+};
+__device__ __forceinline__ LaneAt lane_at(const ScanArgs& a, int col,
+                                          int v) {
+  int64_t lane = (int64_t)col * 64 + (threadIdx.x & 63);
+  LaneAt l;
+  l.on = lane < a.lanes;
+  if (!l.on) lane = a.lanes - 1;
+  l.b = (int)(lane / a.cv);
+  l.ch = (int)(lane % a.cv) * v;
+  l.hc = (int64_t)l.b * a.q.c + l.ch;
+  return l;
+}
+template <int V, int W>
+__device__ __forceinline__ int next_ticket(const ScanArgs& a,
+                                           TileShared<V, W>& sh) {
+  if (a.tiles == 1) return blockIdx.x;
+  if (threadIdx.x == 0)
+    sh.ticket = (int)__hip_atomic_fetch_add((unsigned*)a.ends, 1u,
+                                            __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return sh.ticket;
+}
+// Bit k: a reset before step s0 + k.
+__device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
+                                            int b, int s0) {
+  unsigned m = 0;
+  if (a.q.reset)
+    for (int k = 0; k < kSplit; ++k)
+      if (s0 + k < r.len && reset_at(a.q, r, b, s0 + k)) m |= 1u << k;
+  return m;
+}
+
+template <typename T, typename O, int V, bool GATE, int W>
+__global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
+  __shared__ TileShared<V, W> sh;
+  const int ticket = next_ticket<V, W>(a, sh);
+  const int wave = threadIdx.x / 64;
+  const int tile = ticket / a.cols, col = ticket % a.cols;
+  const LaneAt l = lane_at(a, col, V);
   const Row r = row_of(a.q, l.b);
+  const int64_t plane = (int64_t)a.q.b * a.q.c;
+  const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
   const T* pf = (const T*)a.f.p + (int64_t)l.b * a.f.sb + l.ch;
   const T* po =
       GATE ? (const T*)a.o.p + (int64_t)l.b * a.o.sb + l.ch : nullptr;
-  const O* pd = (const O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
-  float TA[V], TD[V];
+  O* py = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
+  const int s0 = (tile * W + wave) * kSplit;
+  float h[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = tile == 0 && a.h ? a.h[l.hc + e] : 0.f;
+  const bool any = __any(s0 < r.len);
+  float keep[kSplit][V], u[kSplit][V];
+  Pack<T, V> io[kSplit];
+  unsigned cuts = 0;
+  float A[V], H[V], TA[V], TH[V];
+  none<V>(A, H);
+  if (any) {
+    Pack<T, V> iv[kSplit], jf[kSplit];
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k) {
+      const int64_t t = time_in(r, s0 + k);
+      jf[k] = load_pack<T, V>(pf + t * a.f.st);
+      iv[k] = load_pack<T, V>(pv + t * a.v.st);
+    }
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k)
+      if (GATE) io[k] = load_pack<T, V>(po + time_in(r, s0 + k) * a.o.st);
+    cuts = cuts_of(a, r, l.b, s0);
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k) {
+      float v[V], f[V];
+      unpack<T, V>(iv[k], v);
+      unpack<T, V>(jf[k], f);
+      const bool live = s0 + k < r.len, cut = cuts >> k & 1;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float write;
+        sigmoids(f[e], keep[k][e], write);
+        u[k][e] = write * v[e];
+        if (live) {
+          H[e] = __builtin_fmaf(keep[k][e], cut ? 0.f : H[e], u[k][e]);
+          A[e] = cut ? kCut : A[e] * keep[k][e];
+        }
+      }
+    }
+  }
+  join_waves<V, W>(sh, wave, A, H, TA, TH);
+  float WA[V], WH[V];     // what runs before the wave in its tile
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    TA[e] = 1.f;
-    TD[e] = 0.f;
+    WA[e] = A[e];
+    WH[e] = H[e];
   }
-  for (int sub = a.subs - 1; sub >= 0; --sub) {
-    const int s0 = (tile * a.subs + sub) * kRound + wave * kSplit;
-    float A[V], D[V];
+  enter_tile<V, W>(a, sh, tile, col, wave, TA, TH, h);
+  if (tile == a.tiles - 1 && a.h_out && wave == 0 && l.on) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = 1.f;
-      D[e] = 0.f;
-    }
-    if (__any(s0 < r.len)) {
-      Pack<T, V> jf[kSplit], io[kSplit];
-      Pack<O, V> id[kSplit];
+    for (int e = 0; e < V; ++e)
+      a.h_out[l.hc + e] =
+          is_cut(TA[e]) ? TH[e] : __builtin_fmaf(TA[e], h[e], TH[e]);
+  }
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        const int64_t tc = time_in(r, s0 + k);
-        jf[k] = load_pack<T, V>(pf + tc * a.f.st);
-        if (GATE) io[k] = load_pack<T, V>(po + tc * a.o.st);
-        id[k] = load_pack<O, V>(pd + tc * a.y.st);
-      }
+  for (int e = 0; e < V; ++e)
+    h[e] = is_cut(WA[e]) ? WH[e] : __builtin_fmaf(WA[e], h[e], WH[e]);
+  if (!l.on) return;
+  if (any) {
+    if (a.states && s0 < r.len)
+      store_pack<float, V>(a.states + (s0 / kStride) * plane + l.hc, h);
 #pragma unroll
-      for (int k = kSplit - 1; k >= 0; --k) {
-        float f[V], d[V];
-        unpack<T, V>(jf[k], f);
-        unpack<O, V>(id[k], d);
-        const bool live = s0 + k < r.len;
-        const bool cut = live && reset_at(a.q, r, l.b, s0 + k);
+    for (int k = 0; k < kSplit; ++k) {
+      if (s0 + k < r.len) {
+        const bool cut = cuts >> k & 1;
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          h[e] = __builtin_fmaf(keep[k][e], cut ? 0.f : h[e], u[k][e]);
+          y[e] = h[e];
+        }
         if (GATE) {
           float o[V];
           unpack<T, V>(io[k], o);
 #pragma unroll
-          for (int e = 0; e < V; ++e) d[e] *= sigmoid(o[e]);
+          for (int e = 0; e < V; ++e) y[e] *= sigmoid(o[e]);
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float keep = sigmoid(f[e]);
-          D[e] = live ? back(D[e] + d[e], keep, cut) : D[e];
-          A[e] = live ? (cut ? -0.f : A[e] * keep) : A[e];
-        }
+        store_pack<O, V>(py + time_of(r, s0 + k) * a.y.st, y);
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = D[e];
-    }
-    __syncthreads();
-    if (wave == 0)
-      fold_back<V>(&sa[0][at], &sh[0][at], kWaves, 64 * V, TA, TD);
   }
-  if (wave == 0 && l.on) {
-    const int64_t plane = (int64_t)a.q.b * a.q.c;
-    float* o = a.ends + (int64_t)tile * 2 * plane + l.hc;
-    store_pack<float, V>(o, TA);
-    store_pack<float, V>(o + plane, TD);
-    if (tile == 0) {   // a copy: dh may replace it in place
-      float h[V];
+  const int s1 = min(s0 + kSplit, a.q.t);
+  for (int s = max(s0, r.len); s < s1; ++s) {
+    float z[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = a.h ? a.h[l.hc + e] : 0.f;
-      store_pack<float, V>(a.ends + (int64_t)a.tiles * 2 * plane + l.hc, h);
-    }
+    for (int e = 0; e < V; ++e) z[e] = 0.f;
+    store_pack<O, V>(py + (int64_t)s * a.y.st, z);
   }
 }
 
-template <typename T, typename O, int V, bool GATE>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_grad_tiles(ScanArgs a) {
-  __shared__ float sa[kWaves][64 * V], sh[kWaves][64 * V];
-  const int wave = threadIdx.x / 64, at = (threadIdx.x & 63) * V;
-  const int tile = blockIdx.x / a.cols;
-  const LaneAt l = lane_at(a, V);
+// The backward pass: tiles and waves run from the row's last step; the states
+// of a wave's steps come again from the one kept before them.
+template <typename T, typename O, int V, bool GATE, int W>
+__global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
+  __shared__ TileShared<V, W> sh;
+  const int ticket = next_ticket<V, W>(a, sh);
+  const int wave = threadIdx.x / 64;
+  const int k_th = ticket / a.cols, col = ticket % a.cols;
+  const LaneAt l = lane_at(a, col, V);
   const Row r = row_of(a.q, l.b);
   const int64_t plane = (int64_t)a.q.b * a.q.c;
   const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
@@ -576,155 +577,117 @@ __global__ __launch_bounds__(64 * kWaves) void k_scan_grad_tiles(ScanArgs a) {
   T* pdv = (T*)a.dv.p + (int64_t)l.b * a.dv.sb + l.ch;
   T* pdf = (T*)a.df.p + (int64_t)l.b * a.df.sb + l.ch;
   T* pdo = GATE ? (T*)a.d_o.p + (int64_t)l.b * a.d_o.sb + l.ch : nullptr;
-  // what comes back into the tile's last step
+  const int s0 = ((a.tiles - 1 - k_th) * W + W - 1 - wave) * kSplit;
   float dh[V];
-  if (a.tiles == 1) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) dh[e] = a.h ? a.h[l.hc + e] : 0.f;
-  } else {
-    float A[V], D[V];
+  for (int e = 0; e < V; ++e) dh[e] = k_th == 0 && a.h ? a.h[l.hc + e] : 0.f;
+  const bool any = __any(s0 < r.len);
+  float keep[kSplit][V], write[kSplit][V];
+  float g[kSplit][V];     // dy sigmoid(o)
+  float q[kSplit][V];     // h_{s-1} - v
+  unsigned cuts = 0;
+  float A[V], D[V], TA[V], TD[V];
+  none<V>(A, D);
+  if (any) {
+    Pack<T, V> iv[kSplit], jf[kSplit], io[kSplit];
+    Pack<O, V> id[kSplit];
+    float h[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = 1.f;
-      D[e] = 0.f;
-      dh[e] = a.ends[(int64_t)a.tiles * 2 * plane + l.hc + e];
+    for (int k = 0; k < kSplit; ++k) {
+      const int64_t t = time_in(r, s0 + k);
+      iv[k] = load_pack<T, V>(pv + t * a.v.st);
+      jf[k] = load_pack<T, V>(pf + t * a.f.st);
+      if (GATE) io[k] = load_pack<T, V>(po + t * a.o.st);
+      id[k] = load_pack<O, V>(pd + t * a.y.st);
     }
-    const int after = a.tiles - 1 - tile;
-    const int share = (after + kWaves - 1) / kWaves;
-    const int i0 = min(wave * share, after), i1 = min(i0 + share, after);
-    const float* e0 = a.ends + (int64_t)(tile + 1 + i0) * 2 * plane + l.hc;
-    if (i1 > i0) fold_back<V>(e0, e0 + plane, i1 - i0, 2 * plane, A, D);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = D[e];
-    }
-    __syncthreads();
-    fold_back<V>(&sa[0][at], &sh[0][at], kWaves, 64 * V, A, dh);
-  }
-  for (int sub = a.subs - 1; sub >= 0; --sub) {
-    const int s0 = (tile * a.subs + sub) * kRound + wave * kSplit;
-    const bool any = __any(s0 < r.len);
-    Pack<T, V> jf[kSplit];
-    float g[kSplit][V];     // dy sigmoid(o)
-    float q[kSplit][V];     // h_{s-1} - v
-    float A[V], D[V];
+    for (int e = 0; e < V; ++e) h[e] = 0.f;
+    if (s0 < r.len)
+      unpack<float, V>(load_pack<float, V>(
+                           a.states + (s0 / kStride) * plane + l.hc),
+                       h);
+    cuts = cuts_of(a, r, l.b, s0);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = 1.f;
-      D[e] = 0.f;
-    }
-    if (any) {
-      Pack<T, V> iv[kSplit], io[kSplit];
-      Pack<O, V> id[kSplit];
-      float h[V];
+    for (int k = 0; k < kSplit; ++k) {
+      float v[V], f[V], o[V], go[V];
+      unpack<T, V>(iv[k], v);
+      unpack<T, V>(jf[k], f);
+      unpack<O, V>(id[k], g[k]);
+      if (GATE) unpack<T, V>(io[k], o);
+      const bool cut = cuts >> k & 1;
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        const int64_t tc = time_in(r, s0 + k);
-        iv[k] = load_pack<T, V>(pv + tc * a.v.st);
-        jf[k] = load_pack<T, V>(pf + tc * a.f.st);
-        if (GATE) io[k] = load_pack<T, V>(po + tc * a.o.st);
-        id[k] = load_pack<O, V>(pd + tc * a.y.st);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = 0.f;
-      if (s0 < r.len)
-        unpack<float, V>(load_pack<float, V>(
-                             a.states + (s0 / kStride) * plane + l.hc),
-                         h);
-#pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        float v[V], f[V], o[V], go[V];
-        unpack<T, V>(iv[k], v);
-        unpack<T, V>(jf[k], f);
-        unpack<O, V>(id[k], g[k]);
-        if (GATE) unpack<T, V>(io[k], o);
-        const bool live = s0 + k < r.len;
-        const bool cut = live && reset_at(a.q, r, l.b, s0 + k);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          float keep, write;
-          sigmoids(f[e], keep, write);
-          if (cut) h[e] = 0.f;
-          q[k][e] = h[e] - v[e];
-          h[e] = __builtin_fmaf(keep, h[e], write * v[e]);
-          if (GATE) {
-            float p, n;
-            sigmoids(o[e], p, n);
-            go[e] = g[k][e] * h[e] * p * n;
-            g[k][e] *= p;
-          }
-        }
-        if (GATE && live && l.on)
-          store_pack<T, V>(pdo + time_of(r, s0 + k) * a.d_o.st, go);
-      }
-#pragma unroll
-      for (int k = kSplit - 1; k >= 0; --k) {
-        float f[V];
-        unpack<T, V>(jf[k], f);
-        const bool live = s0 + k < r.len;
-        const bool cut = live && reset_at(a.q, r, l.b, s0 + k);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float keep = sigmoid(f[e]);
-          D[e] = live ? back(D[e] + g[k][e], keep, cut) : D[e];
-          A[e] = live ? (cut ? -0.f : A[e] * keep) : A[e];
+      for (int e = 0; e < V; ++e) {
+        sigmoids(f[e], keep[k][e], write[k][e]);
+        if (cut) h[e] = 0.f;
+        q[k][e] = h[e] - v[e];
+        h[e] = __builtin_fmaf(keep[k][e], h[e], write[k][e] * v[e]);
+        if (GATE) {
+          float p, n;
+          sigmoids(o[e], p, n);
+          go[e] = g[k][e] * h[e] * p * n;
+          g[k][e] *= p;
         }
       }
+      if (GATE && s0 + k < r.len && l.on)
+        store_pack<T, V>(pdo + time_of(r, s0 + k) * a.d_o.st, go);
     }
-    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sa[wave][at + e] = A[e];
-      sh[wave][at + e] = D[e];
-    }
-    __syncthreads();
-    float d[V];
+    for (int k = kSplit - 1; k >= 0; --k) {
+      const bool live = s0 + k < r.len, cut = cuts >> k & 1;
 #pragma unroll
-    for (int e = 0; e < V; ++e) d[e] = dh[e];
-    const int later = kWaves - 1 - wave;
-    if (later)
-      fold_back<V>(&sa[wave + 1][at], &sh[wave + 1][at], later, 64 * V, A, d);
-#pragma unroll
-    for (int e = 0; e < V; ++e) dh[e] = d[e];
-    fold_back<V>(&sa[0][at], &sh[0][at], wave + 1, 64 * V, A, dh);
-    if (any && l.on) {
-#pragma unroll
-      for (int k = kSplit - 1; k >= 0; --k) {
-        if (s0 + k < r.len) {
-          const int64_t t = time_of(r, s0 + k);
-          const bool cut = reset_at(a.q, r, l.b, s0 + k);
-          float f[V], gv[V], gf[V];
-          unpack<T, V>(jf[k], f);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float keep, write;
-            sigmoids(f[e], keep, write);
-            d[e] += g[k][e];
-            gv[e] = d[e] * write;
-            gf[e] = d[e] * q[k][e] * (keep * write);
-            d[e] = back(d[e], keep, cut);
-          }
-          store_pack<T, V>(pdv + t * a.dv.st, gv);
-          store_pack<T, V>(pdf + t * a.df.st, gf);
+      for (int e = 0; e < V; ++e) {
+        if (live) {
+          D[e] = cut ? 0.f : (D[e] + g[k][e]) * keep[k][e];
+          A[e] = cut ? kCut : A[e] * keep[k][e];
         }
-      }
-    }
-    if (l.on) {
-      const int s1 = min(s0 + kSplit, a.q.t);
-      for (int s = max(s0, r.len); s < s1; ++s) {
-        float z[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) z[e] = 0.f;
-        store_pack<T, V>(pdv + (int64_t)s * a.dv.st, z);
-        store_pack<T, V>(pdf + (int64_t)s * a.df.st, z);
-        if (GATE) store_pack<T, V>(pdo + (int64_t)s * a.d_o.st, z);
       }
     }
   }
-  if (a.h_out && tile == 0 && wave == 0 && l.on) {
+  join_waves<V, W>(sh, wave, A, D, TA, TD);
+  float WA[V], WD[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) a.h_out[l.hc + e] = dh[e];
+  for (int e = 0; e < V; ++e) {
+    WA[e] = A[e];
+    WD[e] = D[e];
+  }
+  enter_tile<V, W>(a, sh, k_th, col, wave, TA, TD, dh);
+  if (k_th == a.tiles - 1 && a.h_out && wave == 0 && l.on) {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      a.h_out[l.hc + e] =
+          is_cut(TA[e]) ? TD[e] : __builtin_fmaf(TA[e], dh[e], TD[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    dh[e] = is_cut(WA[e]) ? WD[e] : __builtin_fmaf(WA[e], dh[e], WD[e]);
+  if (!l.on) return;
+  if (any) {
+#pragma unroll
+    for (int k = kSplit - 1; k >= 0; --k) {
+      if (s0 + k < r.len) {
+        const int64_t t = time_of(r, s0 + k);
+        const bool cut = cuts >> k & 1;
+        float gv[V], gf[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dh[e] += g[k][e];
+          gv[e] = dh[e] * write[k][e];
+          gf[e] = dh[e] * q[k][e] * (keep[k][e] * write[k][e]);
+          dh[e] = cut ? 0.f : dh[e] * keep[k][e];
+        }
+        store_pack<T, V>(pdv + t * a.dv.st, gv);
+        store_pack<T, V>(pdf + t * a.df.st, gf);
+      }
+    }
+  }
+  const int s1 = min(s0 + kSplit, a.q.t);
+  for (int s = max(s0, r.len); s < s1; ++s) {
+    float z[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) z[e] = 0.f;
+    store_pack<T, V>(pdv + (int64_t)s * a.dv.st, z);
+    store_pack<T, V>(pdf + (int64_t)s * a.df.st, z);
+    if (GATE) store_pack<T, V>(pdo + (int64_t)s * a.d_o.st, z);
   }
 }
 
@@ -752,44 +715,50 @@ void with_scan(int v, bool gate, F&& f) {
 // each.
 constexpr int kSerialSteps = 64;
 constexpr int64_t kFillWaves = 2048;    // eight to a CU
-constexpr int kMaxTiles = 512;
 
 struct ScanCut {
   bool split = false;
-  int cols = 0, tiles = 0, subs = 0;
+  int cols = 0, tiles = 0, group = 0;
+  uint64_t words = 0;
 };
-ScanCut cut_of(const st_seq_desc& d, int v) {
+ScanCut cut_of(const st_seq_desc& d, int v, int waves) {
   ScanCut c;
   const int64_t lanes = (int64_t)d.b * (d.c / v);
   const int64_t cols = ceil_div(lanes, 64);
   if (d.t <= kSerialSteps || cols >= kFillWaves) return c;
   c.split = true;
   c.cols = (int)cols;
-  const int64_t rounds = ceil_div(d.t, kRound);
-  const int64_t want =
-      std::min<int64_t>(kMaxTiles, ceil_div(2 * kFillWaves, cols * kWaves));
-  c.subs = (int)ceil_div(rounds, std::min(rounds, want));
-  c.tiles = (int)ceil_div(rounds, c.subs);
+  c.tiles = (int)ceil_div(d.t, (int64_t)kSplit * waves);
+  // a block folds at most group tiles and tiles / group groups
+  c.group = 8;
+  while ((int64_t)c.group * c.group < c.tiles) c.group *= 2;
+  if (c.tiles > 1)
+    c.words = kHeadWords + (uint64_t)(c.tiles + c.tiles / c.group) * 2 *
+                               c.cols * 64 * v;
   return c;
 }
+constexpr int kWaves = 8, kGradWaves = 8;
 
-uint64_t scan_space(const st_seq_desc& d, bool) {
+uint64_t scan_space(const st_seq_desc& d, bool backward) {
   uint64_t most = 0;
-  for (int v = 4; v >= 1; v /= 2) {
-    if (d.c % v || empty(d)) continue;
-    const ScanCut c = cut_of(d, v);
-    if (c.split && c.tiles > 1)
+  for (int v = 2; v >= 1; v /= 2)
+    if (d.c % v == 0 && !empty(d))
       most = std::max<uint64_t>(
-          most, (uint64_t)(2 * c.tiles + 1) * d.b * d.c * sizeof(float));
-  }
-  return most;
+          most, cut_of(d, v, backward ? kGradWaves : kWaves).words * 8);
+  return (most + 15) / 16 * 16;
 }
 
-void take_cut(ScanArgs& a, const ScanCut& c, void* ws) {
+// Clears the workspace of a launch of split rows.
+void take_cut(ScanArgs& a, const ScanCut& c, void* ws, hipStream_t q) {
   a.cols = c.cols;
   a.tiles = c.tiles;
-  a.subs = c.subs;
-  a.ends = (float*)ws;
+  a.group = c.group;
+  a.ends = ws;
+  if (c.words) {
+    const int64_t n = (int64_t)(c.words + 1) / 2;
+    k_scan_clear<<<(unsigned)std::min<int64_t>(ceil_div(n, 256), 1024), 256,
+                   0, q>>>((uint4*)ws, n);
+  }
 }
 
 }  // namespace
@@ -858,10 +827,17 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.states = states;
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
-    const unsigned grid = (unsigned)ceil_div(a.lanes, kThreads);
-    const ScanCut cut = cut_of(*d, vec);
-    take_cut(a, cut, ws);
     hipStream_t q = (hipStream_t)stream;
+    const ScanCut cut = cut_of(*d, std::min(vec, 2), kWaves);
+    if (cut.split) {
+      vec = std::min(vec, 2);
+      a.cv = d->c / vec;
+      a.lanes = (int64_t)d->b * a.cv;
+      take_cut(a, cut, ws, q);
+    }
+    const unsigned grid =
+        cut.split ? (unsigned)(cut.cols * cut.tiles)
+                  : (unsigned)ceil_div(a.lanes, kThreads);
     with_types(d->dtype, d->out_dtype, [&](auto ti, auto to) {
       using T = typename decltype(ti)::type;
       using O = typename decltype(to)::type;
@@ -872,11 +848,9 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
           k_scan<T, O, V, G><<<grid, kThreads, 0, q>>>(a);
           return;
         }
-        if (cut.tiles > 1)
-          k_scan_ends<T, V>
-              <<<cut.cols * cut.tiles, 64 * kWaves, 0, q>>>(a);
-        k_scan_tiles<T, O, V, G>
-            <<<cut.cols * cut.tiles, 64 * kWaves, 0, q>>>(a);
+        if constexpr (V <= 2)
+          k_scan_tiles<T, O, V, G, kWaves>
+              <<<grid, 64 * kWaves, 0, q>>>(a);
       });
     });
     return launch_status("gated scan");
@@ -957,10 +931,17 @@ extern "C" st_status st_gated_scan_backward(
     a.states = const_cast<float*>(states);
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
-    const unsigned grid = (unsigned)ceil_div(a.lanes, kThreads);
-    const ScanCut cut = cut_of(*d, vec);
-    take_cut(a, cut, ws);
     hipStream_t q = (hipStream_t)stream;
+    const ScanCut cut = cut_of(*d, std::min(vec, 2), kGradWaves);
+    if (cut.split) {
+      vec = std::min(vec, 2);
+      a.cv = d->c / vec;
+      a.lanes = (int64_t)d->b * a.cv;
+      take_cut(a, cut, ws, q);
+    }
+    const unsigned grid =
+        cut.split ? (unsigned)(cut.cols * cut.tiles)
+                  : (unsigned)ceil_div(a.lanes, kThreads);
     with_types(d->dtype, d->out_dtype, [&](auto ti, auto to) {
       using T = typename decltype(ti)::type;
       using O = typename decltype(to)::type;
@@ -971,11 +952,9 @@ extern "C" st_status st_gated_scan_backward(
           k_scan_grad<T, O, V, G><<<grid, kThreads, 0, q>>>(a);
           return;
         }
-        if (cut.tiles > 1)
-          k_scan_grad_ends<T, O, V, G>
-              <<<cut.cols * cut.tiles, 64 * kWaves, 0, q>>>(a);
-        k_scan_grad_tiles<T, O, V, G>
-            <<<cut.cols * cut.tiles, 64 * kWaves, 0, q>>>(a);
+        if constexpr (V <= 2)
+          k_scan_grad_tiles<T, O, V, G, kGradWaves>
+              <<<grid, 64 * kGradWaves, 0, q>>>(a);
       });
     });
     return launch_status("gated scan backward");

@@ -42,12 +42,13 @@ __device__ __forceinline__ void store_pack(T* p, const float* f) {
 }
 
 // e^x for x <= 0, to about an ulp: 2^(x log2 e) with the product's rounding
-// error and the constant's tail brought back in the exponent.
+// error and the constant's tail brought back.  (Below -104 the result is zero;
+// -inf would make the correction NaN.)
 __device__ __forceinline__ float exp_nonpos(float x) {
   const float hi = 1.44269502162933349609f, lo = 1.92596299e-8f;
+  x = x < -104.f ? -104.f : x;   // NaN stays
   const float t = x * hi;
-  // below 2^-126 the result is zero; keeps -inf out of the correction
-  const float r = t > -127.f ? __builtin_fmaf(x, hi, -t) + x * lo : 0.f;
+  const float r = __builtin_fmaf(x, lo, __builtin_fmaf(x, hi, -t));
   const float e = __builtin_amdgcn_exp2f(t);
   return __builtin_fmaf(e * r, 0.693147180559945f, e);
 }
