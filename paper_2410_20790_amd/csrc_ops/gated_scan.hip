@@ -30,6 +30,7 @@ struct ScanArgs {
   int cols;                        // blocks of 64 lanes
   int tiles, group;                // tiles of a row, tiles of a group
   void* ends;                      // the ticket, then words: tiles, groups
+  int narrow;                      // 32-bit offsets within one time
 };
 constexpr int kHeadWords = 2;
 
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(ScanArgs a) {
           float o[V];
           unpack<T, V>(io[k], o);
 #pragma unroll
-          for (int e = 0; e < V; ++e) y[e] *= sigmoid(o[e]);
+          for (int e = 0; e < V; ++e) y[e] *= out_gate<O>(o[e]);
         }
         store_pack<O, V>(py + time_of(r, s + k) * a.y.st, y);
       }
@@ -224,12 +225,6 @@ __device__ __forceinline__ bool is_cut(float A) {
   return __float_as_uint(A) == 0x80000000u;
 }
 
-// The time of step s, or of the row's nearest (time 0 of a row of none).
-__device__ __forceinline__ int64_t time_in(const Row& r, int s) {
-  const int64_t t = time_of(r, max(0, min(s, r.len - 1)));
-  return t < 0 ? 0 : t;
-}
-
 // (A, H), then (x, y): the steps of (x, y) run after those of (A, H).
 template <int V>
 __device__ __forceinline__ void then(float* A, float* H, const float* x,
@@ -276,32 +271,33 @@ __device__ __forceinline__ void put_entry(const Ends& p, int64_t i,
     publish(w + p.plane + e, H[e]);
   }
 }
-// Folds entries [i0, i1) into (A, H), four at a time, waiting for each.
+// Folds entries [i0, i1) into (A, H), two at a time, waiting for each.  (Few
+// registers: the gates of the block's steps are held meanwhile.)
 template <int V>
-__device__ __forceinline__ void fold_entries(const Ends& p, int64_t i0,
-                                             int64_t i1, float* A, float* H) {
-  for (int64_t i = i0; i < i1; i += 4) {
-    Word w[4][2 * V];
+__device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
+                                             float* A, float* H) {
+  const Word* q = p.base + (int64_t)i0 * 2 * p.plane;
+  for (int i = i0; i < i1; i += 2) {
+    const int64_t next = i + 1 < i1 ? 2 * p.plane : 0;
+    Word w[2][2 * V];
     bool all;
     do {
       all = true;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const Word* q = p.base + min(i + k, i1 - 1) * 2 * p.plane;
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          w[k][e] = peek(q + e);
-          w[k][V + e] = peek(q + p.plane + e);
+          w[k][e] = peek(q + k * next + e);
+          w[k][V + e] = peek(q + k * next + p.plane + e);
         }
-      }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) all = all && (w[k][e] >> 32) != 0;
-      if (!all) __builtin_amdgcn_s_sleep(2);
+      if (!all) __builtin_amdgcn_s_sleep(1);
     } while (!all);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       if (i + k < i1) {
         float x[V], y[V];
 #pragma unroll
@@ -312,6 +308,7 @@ __device__ __forceinline__ void fold_entries(const Ends& p, int64_t i0,
         then<V>(A, H, x, y);
       }
     }
+    q += 2 * next;
   }
 }
 
@@ -384,7 +381,7 @@ __device__ __forceinline__ void enter_tile(const ScanArgs& a,
   // the tiles of its group before it, a share to each wave
   none<V>(A, H);
   const int share = (in + W - 1) / W;
-  const int64_t g0 = (int64_t)g * a.group;
+  const int g0 = g * a.group;
   fold_entries<V>(p, g0 + min(wave * share, in),
                   g0 + min((wave + 1) * share, in), A, H);
   join_waves<V, W>(sh, wave, A, H, PA, PH);
@@ -401,8 +398,8 @@ __device__ __forceinline__ void enter_tile(const ScanArgs& a,
   // the groups before its own
   none<V>(A, H);
   const int gs = (g + W - 1) / W;
-  fold_entries<V>(p, (int64_t)a.tiles + min(wave * gs, g),
-                  (int64_t)a.tiles + min((wave + 1) * gs, g), A, H);
+  fold_entries<V>(p, a.tiles + min(wave * gs, g),
+                  a.tiles + min((wave + 1) * gs, g), A, H);
   float GA[V], GH[V];
   join_waves<V, W>(sh, wave, A, H, GA, GH);
   then<V>(GA, GH, PA, PH);
@@ -442,7 +439,42 @@ __device__ __forceinline__ int next_ticket(const ScanArgs& a,
                                             __ATOMIC_RELAXED,
                                             __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  return sh.ticket;
+  return __builtin_amdgcn_readfirstlane(sh.ticket);
+}
+// Whether all lanes of a wave have all of its steps, at the same times, and
+// the time of the first.
+struct Whole {
+  bool on;
+  int64_t t;
+  int dir;
+};
+__device__ __forceinline__ Whole whole_wave(const ScanArgs& a, const Row& r,
+                                            int s0) {
+  Whole w;
+  w.on = a.narrow && !(a.q.lengths && a.q.reverse) &&
+         __all(s0 + kSplit <= r.len);
+  w.t = a.q.reverse ? a.q.t - 1 - s0 : s0;
+  w.dir = a.q.reverse ? -1 : 1;
+  return w;
+}
+template <typename T, int V>
+__device__ __forceinline__ void load_steps(const SeqTensor& x, const Whole& w,
+                                           const Row& r, int b, int ch,
+                                           int s0, Pack<T, V>* out) {
+  if (w.on) {
+    const WaveWalk<const T> p(x, w.t, w.dir, b, ch);
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k) out[k] = load_pack<T, V>(p.at(k));
+  } else {
+    Walk<const T> p(x, r, b, ch, s0);
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k) {
+      out[k] = load_pack<T, V>(p.p);
+      p.advance(k);
+      // one address at a time, not all of them in registers first
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
 }
 // Bit k: a reset before step s0 + k.
 __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
@@ -458,21 +490,17 @@ template <typename T, typename O, int V, bool GATE, int W>
 __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   __shared__ TileShared<V, W> sh;
   const int ticket = next_ticket<V, W>(a, sh);
-  const int wave = threadIdx.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int tile = ticket / a.cols, col = ticket % a.cols;
   const LaneAt l = lane_at(a, col, V);
   const Row r = row_of(a.q, l.b);
   const int64_t plane = (int64_t)a.q.b * a.q.c;
-  const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
-  const T* pf = (const T*)a.f.p + (int64_t)l.b * a.f.sb + l.ch;
-  const T* po =
-      GATE ? (const T*)a.o.p + (int64_t)l.b * a.o.sb + l.ch : nullptr;
-  O* py = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
   const int s0 = (tile * W + wave) * kSplit;
   float h[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) h[e] = tile == 0 && a.h ? a.h[l.hc + e] : 0.f;
   const bool any = __any(s0 < r.len);
+  const Whole whole = whole_wave(a, r, s0);
   float keep[kSplit][V], u[kSplit][V];
   Pack<T, V> io[kSplit];
   unsigned cuts = 0;
@@ -480,32 +508,49 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   none<V>(A, H);
   if (any) {
     Pack<T, V> iv[kSplit], jf[kSplit];
-#pragma unroll
-    for (int k = 0; k < kSplit; ++k) {
-      const int64_t t = time_in(r, s0 + k);
-      jf[k] = load_pack<T, V>(pf + t * a.f.st);
-      iv[k] = load_pack<T, V>(pv + t * a.v.st);
-    }
-#pragma unroll
-    for (int k = 0; k < kSplit; ++k)
-      if (GATE) io[k] = load_pack<T, V>(po + time_in(r, s0 + k) * a.o.st);
+    load_steps<T, V>(a.f, whole, r, l.b, l.ch, s0, jf);
+    load_steps<T, V>(a.v, whole, r, l.b, l.ch, s0, iv);
+    if (GATE) load_steps<T, V>(a.o, whole, r, l.b, l.ch, s0, io);
     cuts = cuts_of(a, r, l.b, s0);
 #pragma unroll
     for (int k = 0; k < kSplit; ++k) {
       float v[V], f[V];
       unpack<T, V>(iv[k], v);
       unpack<T, V>(jf[k], f);
-      const bool live = s0 + k < r.len, cut = cuts >> k & 1;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         float write;
         sigmoids(f[e], keep[k][e], write);
         u[k][e] = write * v[e];
-        if (live) {
+      }
+    }
+    // steps behind the row's end keep the state, to the bit
+    if (!whole.on) {
+#pragma unroll
+      for (int k = 0; k < kSplit; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          keep[k][e] = s0 + k < r.len ? keep[k][e] : 1.f;
+          u[k][e] = s0 + k < r.len ? u[k][e] : 0.f;
+        }
+    }
+    if (__any(cuts != 0)) {
+#pragma unroll
+      for (int k = 0; k < kSplit; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const bool cut = cuts >> k & 1;
           H[e] = __builtin_fmaf(keep[k][e], cut ? 0.f : H[e], u[k][e]);
           A[e] = cut ? kCut : A[e] * keep[k][e];
         }
-      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kSplit; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          H[e] = __builtin_fmaf(keep[k][e], H[e], u[k][e]);
+          A[e] *= keep[k][e];
+        }
     }
   }
   join_waves<V, W>(sh, wave, A, H, TA, TH);
@@ -529,6 +574,8 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   if (any) {
     if (a.states && s0 < r.len)
       store_pack<float, V>(a.states + (s0 / kStride) * plane + l.hc, h);
+    Walk<O> wy(a.y, r, l.b, l.ch, s0);
+    const WaveWalk<O> ww(a.y, whole.t, whole.dir, l.b, l.ch);
 #pragma unroll
     for (int k = 0; k < kSplit; ++k) {
       if (s0 + k < r.len) {
@@ -536,19 +583,26 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
         float y[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          h[e] = __builtin_fmaf(keep[k][e], cut ? 0.f : h[e], u[k][e]);
+          if (cut) h[e] = 0.f;
+          h[e] = __builtin_fmaf(keep[k][e], h[e], u[k][e]);
           y[e] = h[e];
         }
         if (GATE) {
           float o[V];
           unpack<T, V>(io[k], o);
 #pragma unroll
-          for (int e = 0; e < V; ++e) y[e] *= sigmoid(o[e]);
+          for (int e = 0; e < V; ++e) y[e] *= out_gate<O>(o[e]);
         }
-        store_pack<O, V>(py + time_of(r, s0 + k) * a.y.st, y);
+        if (whole.on) {
+          store_pack<O, V>(ww.at(k), y);
+        } else {
+          store_pack<O, V>(wy.p, y);
+          wy.advance(k);
+        }
       }
     }
   }
+  O* py = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
   const int s1 = min(s0 + kSplit, a.q.t);
   for (int s = max(s0, r.len); s < s1; ++s) {
     float z[V];
@@ -564,24 +618,17 @@ template <typename T, typename O, int V, bool GATE, int W>
 __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
   __shared__ TileShared<V, W> sh;
   const int ticket = next_ticket<V, W>(a, sh);
-  const int wave = threadIdx.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int k_th = ticket / a.cols, col = ticket % a.cols;
   const LaneAt l = lane_at(a, col, V);
   const Row r = row_of(a.q, l.b);
   const int64_t plane = (int64_t)a.q.b * a.q.c;
-  const T* pv = (const T*)a.v.p + (int64_t)l.b * a.v.sb + l.ch;
-  const T* pf = (const T*)a.f.p + (int64_t)l.b * a.f.sb + l.ch;
-  const T* po =
-      GATE ? (const T*)a.o.p + (int64_t)l.b * a.o.sb + l.ch : nullptr;
-  const O* pd = (const O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
-  T* pdv = (T*)a.dv.p + (int64_t)l.b * a.dv.sb + l.ch;
-  T* pdf = (T*)a.df.p + (int64_t)l.b * a.df.sb + l.ch;
-  T* pdo = GATE ? (T*)a.d_o.p + (int64_t)l.b * a.d_o.sb + l.ch : nullptr;
   const int s0 = ((a.tiles - 1 - k_th) * W + W - 1 - wave) * kSplit;
   float dh[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) dh[e] = k_th == 0 && a.h ? a.h[l.hc + e] : 0.f;
   const bool any = __any(s0 < r.len);
+  const Whole whole = whole_wave(a, r, s0);
   float keep[kSplit][V], write[kSplit][V];
   float g[kSplit][V];     // dy sigmoid(o)
   float q[kSplit][V];     // h_{s-1} - v
@@ -592,14 +639,10 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
     Pack<T, V> iv[kSplit], jf[kSplit], io[kSplit];
     Pack<O, V> id[kSplit];
     float h[V];
-#pragma unroll
-    for (int k = 0; k < kSplit; ++k) {
-      const int64_t t = time_in(r, s0 + k);
-      iv[k] = load_pack<T, V>(pv + t * a.v.st);
-      jf[k] = load_pack<T, V>(pf + t * a.f.st);
-      if (GATE) io[k] = load_pack<T, V>(po + t * a.o.st);
-      id[k] = load_pack<O, V>(pd + t * a.y.st);
-    }
+    load_steps<T, V>(a.f, whole, r, l.b, l.ch, s0, jf);
+    load_steps<T, V>(a.v, whole, r, l.b, l.ch, s0, iv);
+    if (GATE) load_steps<T, V>(a.o, whole, r, l.b, l.ch, s0, io);
+    load_steps<O, V>(a.y, whole, r, l.b, l.ch, s0, id);
 #pragma unroll
     for (int e = 0; e < V; ++e) h[e] = 0.f;
     if (s0 < r.len)
@@ -607,6 +650,8 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
                            a.states + (s0 / kStride) * plane + l.hc),
                        h);
     cuts = cuts_of(a, r, l.b, s0);
+    Walk<T> wg(GATE ? a.d_o : a.dv, r, l.b, l.ch, s0);
+    const WaveWalk<T> wwg(GATE ? a.d_o : a.dv, whole.t, whole.dir, l.b, l.ch);
 #pragma unroll
     for (int k = 0; k < kSplit; ++k) {
       float v[V], f[V], o[V], go[V];
@@ -628,19 +673,41 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
           g[k][e] *= p;
         }
       }
-      if (GATE && s0 + k < r.len && l.on)
-        store_pack<T, V>(pdo + time_of(r, s0 + k) * a.d_o.st, go);
+      if (GATE && s0 + k < r.len && l.on) {
+        if (whole.on) {
+          store_pack<T, V>(wwg.at(k), go);
+        } else {
+          store_pack<T, V>(wg.p, go);
+          wg.advance(k);
+        }
+      }
     }
+    if (!whole.on) {
 #pragma unroll
-    for (int k = kSplit - 1; k >= 0; --k) {
-      const bool live = s0 + k < r.len, cut = cuts >> k & 1;
+      for (int k = 0; k < kSplit; ++k)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        if (live) {
+        for (int e = 0; e < V; ++e) {
+          keep[k][e] = s0 + k < r.len ? keep[k][e] : 1.f;
+          g[k][e] = s0 + k < r.len ? g[k][e] : 0.f;
+        }
+    }
+    if (__any(cuts != 0)) {
+#pragma unroll
+      for (int k = kSplit - 1; k >= 0; --k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const bool cut = cuts >> k & 1;
           D[e] = cut ? 0.f : (D[e] + g[k][e]) * keep[k][e];
           A[e] = cut ? kCut : A[e] * keep[k][e];
         }
-      }
+    } else {
+#pragma unroll
+      for (int k = kSplit - 1; k >= 0; --k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          D[e] = (D[e] + g[k][e]) * keep[k][e];
+          A[e] *= keep[k][e];
+        }
     }
   }
   join_waves<V, W>(sh, wave, A, D, TA, TD);
@@ -662,10 +729,14 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
     dh[e] = is_cut(WA[e]) ? WD[e] : __builtin_fmaf(WA[e], dh[e], WD[e]);
   if (!l.on) return;
   if (any) {
+    // back from the last of the wave's steps that the row has
+    Walk<T> wv(a.dv, r, l.b, l.ch, s0 + kSplit - 1),
+        wf(a.df, r, l.b, l.ch, s0 + kSplit - 1);
+    const WaveWalk<T> wwv(a.dv, whole.t, whole.dir, l.b, l.ch),
+        wwf(a.df, whole.t, whole.dir, l.b, l.ch);
 #pragma unroll
     for (int k = kSplit - 1; k >= 0; --k) {
       if (s0 + k < r.len) {
-        const int64_t t = time_of(r, s0 + k);
         const bool cut = cuts >> k & 1;
         float gv[V], gf[V];
 #pragma unroll
@@ -675,11 +746,21 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
           gf[e] = dh[e] * q[k][e] * (keep[k][e] * write[k][e]);
           dh[e] = cut ? 0.f : dh[e] * keep[k][e];
         }
-        store_pack<T, V>(pdv + t * a.dv.st, gv);
-        store_pack<T, V>(pdf + t * a.df.st, gf);
+        if (whole.on) {
+          store_pack<T, V>(wwv.at(k), gv);
+          store_pack<T, V>(wwf.at(k), gf);
+        } else {
+          store_pack<T, V>(wv.p, gv);
+          store_pack<T, V>(wf.p, gf);
+          wv.p -= wv.step;
+          wf.p -= wf.step;
+        }
       }
     }
   }
+  T* pdv = (T*)a.dv.p + (int64_t)l.b * a.dv.sb + l.ch;
+  T* pdf = (T*)a.df.p + (int64_t)l.b * a.df.sb + l.ch;
+  T* pdo = GATE ? (T*)a.d_o.p + (int64_t)l.b * a.d_o.sb + l.ch : nullptr;
   const int s1 = min(s0 + kSplit, a.q.t);
   for (int s = max(s0, r.len); s < s1; ++s) {
     float z[V];
@@ -721,10 +802,9 @@ struct ScanCut {
   int cols = 0, tiles = 0, group = 0;
   uint64_t words = 0;
 };
-ScanCut cut_of(const st_seq_desc& d, int v, int waves) {
+ScanCut cut_of(const st_seq_desc& d, int waves) {
   ScanCut c;
-  const int64_t lanes = (int64_t)d.b * (d.c / v);
-  const int64_t cols = ceil_div(lanes, 64);
+  const int64_t cols = ceil_div((int64_t)d.b * d.c, 64);
   if (d.t <= kSerialSteps || cols >= kFillWaves) return c;
   c.split = true;
   c.cols = (int)cols;
@@ -734,18 +814,14 @@ ScanCut cut_of(const st_seq_desc& d, int v, int waves) {
   while ((int64_t)c.group * c.group < c.tiles) c.group *= 2;
   if (c.tiles > 1)
     c.words = kHeadWords + (uint64_t)(c.tiles + c.tiles / c.group) * 2 *
-                               c.cols * 64 * v;
+                               c.cols * 64;
   return c;
 }
 constexpr int kWaves = 8, kGradWaves = 8;
 
 uint64_t scan_space(const st_seq_desc& d, bool backward) {
-  uint64_t most = 0;
-  for (int v = 2; v >= 1; v /= 2)
-    if (d.c % v == 0 && !empty(d))
-      most = std::max<uint64_t>(
-          most, cut_of(d, v, backward ? kGradWaves : kWaves).words * 8);
-  return (most + 15) / 16 * 16;
+  if (empty(d)) return 0;
+  return (cut_of(d, backward ? kGradWaves : kWaves).words * 8 + 15) / 16 * 16;
 }
 
 // Clears the workspace of a launch of split rows.
@@ -822,17 +898,19 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.f = tensor_of(f);
     a.o = tensor_of(o);
     a.y = tensor_of(y);
+    a.narrow = narrow(*d, v, es) && narrow(*d, f, es) && narrow(*d, o, es) &&
+               narrow(*d, y, eo);
     a.h = h;
     a.h_out = h_out;
     a.states = states;
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, std::min(vec, 2), kWaves);
+    const ScanCut cut = cut_of(*d, kWaves);
     if (cut.split) {
-      vec = std::min(vec, 2);
-      a.cv = d->c / vec;
-      a.lanes = (int64_t)d->b * a.cv;
+      vec = 1;
+      a.cv = d->c;
+      a.lanes = (int64_t)d->b * d->c;
       take_cut(a, cut, ws, q);
     }
     const unsigned grid =
@@ -848,7 +926,7 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
           k_scan<T, O, V, G><<<grid, kThreads, 0, q>>>(a);
           return;
         }
-        if constexpr (V <= 2)
+        if constexpr (V == 1)
           k_scan_tiles<T, O, V, G, kWaves>
               <<<grid, 64 * kWaves, 0, q>>>(a);
       });
@@ -926,17 +1004,20 @@ extern "C" st_status st_gated_scan_backward(
     a.dv = tensor_of(dv);
     a.df = tensor_of(df);
     a.d_o = tensor_of(d_o);
+    a.narrow = narrow(*d, dy, eo);
+    for (const st_seq_ref* r : {v, f, o, dv, df, d_o})
+      a.narrow = a.narrow && narrow(*d, r, es);
     a.h = dh_out;
     a.h_out = dh;
     a.states = const_cast<float*>(states);
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, std::min(vec, 2), kGradWaves);
+    const ScanCut cut = cut_of(*d, kGradWaves);
     if (cut.split) {
-      vec = std::min(vec, 2);
-      a.cv = d->c / vec;
-      a.lanes = (int64_t)d->b * a.cv;
+      vec = 1;
+      a.cv = d->c;
+      a.lanes = (int64_t)d->b * d->c;
       take_cut(a, cut, ws, q);
     }
     const unsigned grid =
@@ -952,7 +1033,7 @@ extern "C" st_status st_gated_scan_backward(
           k_scan_grad<T, O, V, G><<<grid, kThreads, 0, q>>>(a);
           return;
         }
-        if constexpr (V <= 2)
+        if constexpr (V == 1)
           k_scan_grad_tiles<T, O, V, G, kGradWaves>
               <<<grid, 64 * kGradWaves, 0, q>>>(a);
       });

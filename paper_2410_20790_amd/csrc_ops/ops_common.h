@@ -72,6 +72,21 @@ __device__ __forceinline__ float sigmoid(float x) {
   return p;
 }
 
+// sigmoid(x) where it only scales a value that is then rounded to two bytes:
+// the exponent's and the reciprocal's own errors, some 2^-23 (1 + |x| / 2)
+// relative, lie far below that rounding, 2^-12 at best.
+__device__ __forceinline__ float sigmoid_rough(float x) {
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+  return __builtin_amdgcn_rcpf(1.f + e);
+}
+template <typename O>
+__device__ __forceinline__ float out_gate(float x) {
+  if constexpr (sizeof(O) == 2)
+    return sigmoid_rough(x);
+  else
+    return sigmoid(x);
+}
+
 // f(z) and its derivative for the activation ACT (ST_ACT_*).
 template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {

@@ -45,8 +45,53 @@ __device__ __forceinline__ bool reset_at(const SeqAxes& q, const Row& r,
   return q.reset && q.reset[time_of(r, s) * q.b + b] != 0;
 }
 
+// A row's elements in running order, from step s0 on: advance() goes to the
+// next step, or stays where the row ends (an address that may be read, time 0
+// of a row of no steps).  One addition per step; the products that a time and
+// its stride make up are formed once.
+template <typename T>
+struct Walk {
+  T* p;
+  int64_t step;
+  int left;    // steps that may follow
+  __device__ __forceinline__ Walk(const SeqTensor& x, const Row& r, int b,
+                                  int ch, int s0) {
+    const int last = max(r.len - 1, 0), s = min(s0, last);
+    const int64_t t = r.len > 0 ? time_of(r, s) : 0;
+    p = (T*)x.p + t * x.st + (int64_t)b * x.sb + ch;
+    step = r.dir * x.st;
+    left = last - s;
+  }
+  __device__ __forceinline__ void advance(int k) {  // from step s0 + k
+    if (k < left) p += step;
+  }
+};
+
+// The same for a whole wave whose lanes all have the steps at one time: a
+// scalar address that moves by steps and one 32-bit offset per lane, so that
+// the addresses of many loads in flight take no vector registers.
+template <typename T>
+struct WaveWalk {
+  char* p;
+  int64_t step;
+  uint32_t off;
+  __device__ __forceinline__ WaveWalk(const SeqTensor& x, int64_t t, int dir,
+                                      int b, int ch) {
+    p = (char*)x.p + t * x.st * (int64_t)sizeof(T);
+    step = dir * x.st * (int64_t)sizeof(T);
+    off = (uint32_t)(((int64_t)b * x.sb + ch) * (int64_t)sizeof(T));
+  }
+  __device__ __forceinline__ T* at(int k) const {
+    return (T*)(p + k * step + off);
+  }
+};
+
 // -------------------------------------------------------------- host side
 
+// Whether a lane's offset within one time of the tensor fits 32 bits.
+inline bool narrow(const st_seq_desc& d, const st_seq_ref* r, int es) {
+  return !r || ((int64_t)(d.b - 1) * r->stride_b + d.c) * es < (int64_t)1 << 31;
+}
 inline SeqAxes axes_of(const st_seq_desc& d) {
   return SeqAxes{d.t, d.b, d.c, d.reverse != 0, d.lengths, d.reset};
 }

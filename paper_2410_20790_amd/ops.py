@@ -26,22 +26,33 @@ def _require(ok, msg):
         raise ValueError(msg)
 
 
+# The checks below run on every call, beside kernels of a few microseconds:
+# their messages are only put together when one fails.
+
 def _code(x, name):
-    _require(isinstance(x, torch.Tensor) and x.is_cuda,
-             f"{name} must be a device tensor")
-    _require(x.dtype in _CODES, f"{name} must be float32, float16 or bfloat16")
-    return _CODES[x.dtype]
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    return code
+
+
+def _mismatch(name, shape, dtype, device, contiguous=False):
+    return ValueError(
+        f"{name} must be a {'contiguous ' if contiguous else ''}tensor "
+        f"{tuple(shape)}{'' if dtype is None else ' of ' + str(dtype)} on "
+        f"{device}")
 
 
 def _plain(x, shape, dtype, device, name):
     """Address of a contiguous tensor that may be absent."""
     if x is None:
         return None
-    _require(isinstance(x, torch.Tensor) and x.device == device
-             and x.dtype == dtype and tuple(x.shape) == tuple(shape)
-             and x.is_contiguous(),
-             f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on "
-             f"{device}")
+    if (not isinstance(x, torch.Tensor) or x.dtype != dtype
+            or x.shape != shape or x.device != device
+            or not x.is_contiguous()):
+        raise _mismatch(name, shape, dtype, device, True)
     return x.data_ptr()
 
 
@@ -57,43 +68,54 @@ def _out_dtype(x, out, out_dtype):
     return out_dtype
 
 
-def _workspace(nbytes, device):
+def _workspace(x, nbytes):
+    """A workspace beside x, and its address."""
     if not nbytes:
         return None, None
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
     return ws, ws.data_ptr()
 
 
 class _On:
-    """Makes the tensors' device current for a call, where it is not."""
+    """Makes the tensors' device current for a call, where it is not, and
+    gives its current stream."""
+    __slots__ = ("index", "back")
 
     def __init__(self, device):
-        self.device, self.back = device.index, None
+        self.index, self.back = device.index, None
 
     def __enter__(self):
         now = torch.cuda.current_device()
-        if now != self.device:
+        if now != self.index:
             self.back = now
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream().cuda_stream
+            torch.cuda.set_device(self.index)
+        return _stream_of(self.index)
 
     def __exit__(self, *exc):
         if self.back is not None:
             torch.cuda.set_device(self.back)
 
 
+def _stream_object(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the current stream's handle without a stream object around it (an eighth of
+# a small call's time on the host), where torch offers it
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
+
+
 # -------------------------------------------------------------- group norm
 
 def _map(x, shape, device, name, dtype=None):
     """Reference of a channels-last map of `shape` ([n, ..., c])."""
-    _require(isinstance(x, torch.Tensor) and x.device == device
-             and tuple(x.shape) == tuple(shape)
-             and (dtype is None or x.dtype == dtype),
-             f"{name} must be a tensor {tuple(shape)}"
-             f"{'' if dtype is None else ' of ' + str(dtype)} on {device}")
+    if (not isinstance(x, torch.Tensor) or x.shape != shape
+            or x.device != device
+            or (dtype is not None and x.dtype != dtype)):
+        raise _mismatch(name, shape, dtype, device)
     st = x.stride()
-    _require(shape[-1] == 1 or st[-1] == 1,
-             f"{name}: channels must be adjacent")
+    if st[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{name}: channels must be adjacent")
     if len(shape) == 4:
         return B.st_map_ref(x.data_ptr(), st[0], st[1], st[2])
     return B.st_map_ref(x.data_ptr(), st[0], st[1], st[1])
@@ -120,13 +142,12 @@ def group_norm(x, groups, gamma=None, beta=None, act=0, eps=1e-5,
     g = _plain(gamma, (c,), torch.float32, dev, "gamma")
     b = _plain(beta, (c,), torch.float32, dev, "beta")
     xr = _map(x, x.shape, dev, "x")
-    y = torch.empty(x.shape, dtype=dt, device=dev) if out is None else out
+    y = x.new_empty(x.shape, dtype=dt) if out is None else out
     yr = _map(y, x.shape, dev, "out")
-    stats = torch.empty((2, x.shape[0], groups), dtype=torch.float32,
-                        device=dev)
+    stats = x.new_empty((2, x.shape[0], groups), dtype=torch.float32)
     mean, rstd = stats.unbind(0)
     n = B.st_group_norm_workspace(d, 0)
-    ws, wp = _workspace(n, dev)
+    ws, wp = _workspace(x, n)
     with _On(dev) as stream:
         B.st_group_norm(d, xr, g, b, yr, mean.data_ptr(), rstd.data_ptr(),
                         wp, n, stream)
@@ -148,16 +169,16 @@ def group_norm_backward(dy, x, groups, mean, rstd, gamma=None, beta=None,
     r = _plain(rstd, (x.shape[0], groups), torch.float32, dev, "rstd")
     xr = _map(x, x.shape, dev, "x")
     dyr = _map(dy, x.shape, dev, "dy")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None \
+    dx = x.new_empty(x.shape, dtype=x.dtype) if out is None \
         else out
     dxr = _map(dx, x.shape, dev, "out", x.dtype)
     dgamma = dbeta = gp = bp = None
     if need_params:
-        grads = torch.empty((2, c), dtype=torch.float32, device=dev)
+        grads = x.new_empty((2, c), dtype=torch.float32)
         dgamma, dbeta = grads.unbind(0)
         gp, bp = dgamma.data_ptr(), dbeta.data_ptr()
     n = B.st_group_norm_workspace(d, 1)
-    ws, wp = _workspace(n, dev)
+    ws, wp = _workspace(x, n)
     with _On(dev) as stream:
         B.st_group_norm_backward(d, dyr, xr, m, r, g, b, dxr, gp, bp, wp, n,
                                  stream)
@@ -168,14 +189,13 @@ def group_norm_backward(dy, x, groups, mean, rstd, gamma=None, beta=None,
 
 def _seq(x, shape, device, name, dtype=None):
     """Reference of a sequence tensor of `shape` ([t, b, c])."""
-    _require(isinstance(x, torch.Tensor) and x.device == device
-             and tuple(x.shape) == tuple(shape)
-             and (dtype is None or x.dtype == dtype),
-             f"{name} must be a tensor {tuple(shape)}"
-             f"{'' if dtype is None else ' of ' + str(dtype)} on {device}")
+    if (not isinstance(x, torch.Tensor) or x.shape != shape
+            or x.device != device
+            or (dtype is not None and x.dtype != dtype)):
+        raise _mismatch(name, shape, dtype, device)
     st = x.stride()
-    _require(shape[-1] == 1 or st[-1] == 1,
-             f"{name}: channels must be adjacent")
+    if st[2] != 1 and shape[2] != 1:
+        raise ValueError(f"{name}: channels must be adjacent")
     return B.st_seq_ref(x.data_ptr(), st[0], st[1])
 
 
@@ -210,10 +230,10 @@ def time_conv(x, weight, bias=None, act=0, window=None, lengths=None,
     bp = _plain(bias, (c,), torch.float32, dev, "bias")
     win = _plain(window, (k - 1, b, c), x.dtype, dev, "window")
     xr = _seq(x, x.shape, dev, "x")
-    y = torch.empty(x.shape, dtype=dt, device=dev) if out is None else out
+    y = x.new_empty(x.shape, dtype=dt) if out is None else out
     yr = _seq(y, x.shape, dev, "out")
     if window_out is None:
-        window_out = torch.empty((k - 1, b, c), dtype=x.dtype, device=dev)
+        window_out = x.new_empty((k - 1, b, c))
     wo = _plain(window_out, (k - 1, b, c), x.dtype, dev, "window_out")
     with _On(dev) as stream:
         B.st_time_conv(d, k, act, xr, w, bp, win, yr, wo, None, 0, stream)
@@ -240,17 +260,17 @@ def time_conv_backward(dy, x, weight, bias=None, act=0, window=None,
     dwo = _plain(dwindow_out, (k - 1, b, c), x.dtype, dev, "dwindow_out")
     xr = _seq(x, x.shape, dev, "x")
     dyr = _seq(dy, x.shape, dev, "dy")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None \
+    dx = x.new_empty(x.shape, dtype=x.dtype) if out is None \
         else out
     dxr = _seq(dx, x.shape, dev, "out", x.dtype)
-    dwin = torch.empty((k - 1, b, c), dtype=x.dtype, device=dev)
+    dwin = x.new_empty((k - 1, b, c))
     dw = db = dwp = dbp = None
     if need_params:
-        grads = torch.empty((k + 1, c), dtype=torch.float32, device=dev)
+        grads = x.new_empty((k + 1, c), dtype=torch.float32)
         dw, db = grads[:k], grads[k]
         dwp, dbp = dw.data_ptr(), db.data_ptr()
     n = B.st_time_conv_workspace(d, k, 1)
-    ws, wp = _workspace(n, dev)
+    ws, wp = _workspace(x, n)
     with _On(dev) as stream:
         B.st_time_conv_backward(d, k, act, dyr, xr, w, bp, win, dwo, dxr, dwp,
                                 dbp, dwin.data_ptr(), wp, n, stream)
@@ -277,14 +297,14 @@ def gated_scan(v, f, o=None, h=None, lengths=None, reset=None, reverse=False,
     fr = _seq(f, v.shape, dev, "f", v.dtype)
     orf = None if o is None else _seq(o, v.shape, dev, "o", v.dtype)
     hp = _plain(h, (b, c), torch.float32, dev, "h")
-    y = torch.empty(v.shape, dtype=dt, device=dev) if out is None else out
+    y = v.new_empty(v.shape, dtype=dt) if out is None else out
     yr = _seq(y, v.shape, dev, "out")
     if h_out is None:
-        h_out = torch.empty((b, c), dtype=torch.float32, device=dev)
+        h_out = v.new_empty((b, c), dtype=torch.float32)
     ho = _plain(h_out, (b, c), torch.float32, dev, "h_out")
     states = kept_states(t, b, c, dev) if save else None
     n = B.st_gated_scan_workspace(d, 0)
-    ws, wp = _workspace(n, dev)
+    ws, wp = _workspace(v, n)
     with _On(dev) as stream:
         B.st_gated_scan(d, vr, fr, orf, hp, yr, ho,
                         states.data_ptr() if save else None, wp, n, stream)
@@ -310,7 +330,7 @@ def gated_scan_backward(dy, v, f, o=None, *, states, dh=None, lengths=None,
                 "states")
     dho = _plain(dh, (b, c), torch.float32, dev, "dh")
     if out is None:
-        out = [torch.empty(v.shape, dtype=v.dtype, device=dev)
+        out = [v.new_empty(v.shape, dtype=v.dtype)
                for _ in range(2 if o is None else 3)]
     _require(len(out) in (2, 3), "out must hold dv, df and do")
     dv, df = out[0], out[1]
@@ -319,9 +339,9 @@ def gated_scan_backward(dy, v, f, o=None, *, states, dh=None, lengths=None,
     dvr = _seq(dv, v.shape, dev, "dv", v.dtype)
     dfr = _seq(df, v.shape, dev, "df", v.dtype)
     dor = None if o is None else _seq(do, v.shape, dev, "do", v.dtype)
-    dhi = torch.empty((b, c), dtype=torch.float32, device=dev)
+    dhi = v.new_empty((b, c), dtype=torch.float32)
     n = B.st_gated_scan_workspace(d, 1)
-    ws, wp = _workspace(n, dev)
+    ws, wp = _workspace(v, n)
     with _On(dev) as stream:
         B.st_gated_scan_backward(d, dyr, vr, fr, orf, sp, dho, dvr, dfr, dor,
                                  dhi.data_ptr(), wp, n, stream)
