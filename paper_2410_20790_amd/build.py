@@ -34,6 +34,7 @@ SOURCES = [
     ("st_gather.hip", DEVICE),
     ("st_exec.hip", DEVICE),
     ("../csrc_ops/norm.hip", EXACT),
+    ("../csrc_ops/norm_grad.hip", EXACT),
     ("../csrc_ops/time_conv.hip", EXACT),
     ("../csrc_ops/time_conv_grad.hip", EXACT),
     ("../csrc_ops/gated_scan.hip", EXACT),

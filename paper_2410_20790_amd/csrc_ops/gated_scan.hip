@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(ScanArgs a) {
           float o[V];
           unpack<T, V>(io[k], o);
 #pragma unroll
-          for (int e = 0; e < V; ++e) y[e] *= out_gate<O>(o[e]);
+          for (int e = 0; e < V; ++e) y[e] *= sigmoid_once(o[e]);
         }
         store_pack<O, V>(py + time_of(r, s + k) * a.y.st, y);
       }
@@ -591,7 +591,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
           float o[V];
           unpack<T, V>(io[k], o);
 #pragma unroll
-          for (int e = 0; e < V; ++e) y[e] *= out_gate<O>(o[e]);
+          for (int e = 0; e < V; ++e) y[e] *= sigmoid_once(o[e]);
         }
         if (whole.on) {
           store_pack<O, V>(ww.at(k), y);

@@ -1,117 +1,20 @@
-// Group norm with an activation on channels-last maps, forward and backward.
+// Group norm with an activation on channels-last maps, forward, and the host
+// side of both directions.
 //
 //   mean, var over an image's sites and the c / groups channels of a group
-//   xh = (x - mean) rstd,  z = xh gamma + beta,  y = act(z)
-//   dz = dy act'(z);  s1 = mean(dz gamma), s2 = mean(dz gamma xh) per group
-//   dx = rstd (dz gamma - s1 - xh s2);  dgamma = sum dz xh, dbeta = sum dz
+//   y = act((x - mean) rstd gamma + beta)
 //
-// About ten (backward twenty) operations per element moved: bound by memory.
-// The channels of a site are adjacent, so a block takes `cols` vectors of V
-// adjacent channels of `rows` sites at a time, and a thread meets the same
-// channels at every site: their parameters stay in its registers.
+// About ten operations per element moved: bound by memory.
 #include <algorithm>
-#include <numeric>
 
-#include "ops_common.h"
+#include "norm.h"
 
 namespace st {
 namespace ops {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kBatch = 4;        // sites whose loads a thread has in flight
-constexpr int kMaxDirectParts = 64;
-
-// How the channels are cut.  A column block holds whole groups, or (groups
-// wider than a block) one of `cparts` parts of one group.
-struct NormGeom {
-  int64_t sites;       // per image
-  int h1;              // the sites of an image are w steps of stride_w
-  int w;
-  int n, c, groups, cpg;
-  int v;               // channels per vector
-  int whole;           // every vector lies in one group
-  int cv;              // vectors per site
-  int cols, rows;      // vectors and sites a block takes at a time
-  int colblocks, kg, cparts, unit_vec;
-  int slabs;           // site ranges per image, per column block
-  int64_t slab_sites;
-  int64_t units;       // n * slabs * colblocks
-};
-
-struct NormArgs {
-  NormGeom g;
-  const void* x;
-  const void* dy;
-  void* y;             // y or dx
-  int64_t xn, xh, xw, yn, yh, yw, dn, dh, dw;
-  const float* gamma;
-  const float* beta;
-  const float* mean;   // [n][groups]
-  const float* rstd;
-  float* mean_out;
-  float* rstd_out;
-  float eps;
-  float* part;         // forward: [n][groups][parts] {count, mean, M2};
-                       // backward: [n][slabs][c] {sum dz, sum dz xh}
-  int parts;
-  float* chsum;        // backward: [n][c] {sum dz, sum dz xh}
-  float* gsum;         // backward: [n][groups] {s1, s2}
-  float* dgamma;
-  float* dbeta;
-  int dblocks;         // blocks of the last pass that reduce dgamma, dbeta
-};
-
-// The block's place: image, site range, vectors and groups.
-struct Place {
-  int n, slab, cb, vec0, nvec, g0, ng;
-  int64_t s0, s1;
-};
-__device__ __forceinline__ Place place_of(const NormGeom& g, int64_t u) {
-  Place p;
-  p.cb = (int)(u % g.colblocks);
-  const int64_t r = u / g.colblocks;
-  p.slab = (int)(r % g.slabs);
-  p.n = (int)(r / g.slabs);
-  p.s0 = p.slab * g.slab_sites;
-  p.s1 = p.s0 + g.slab_sites < g.sites ? p.s0 + g.slab_sites : g.sites;
-  if (g.cparts == 1) {
-    p.vec0 = p.cb * g.cols;
-    p.nvec = min(g.cols, g.cv - p.vec0);
-    p.g0 = p.cb * g.kg;
-    p.ng = min(g.kg, g.groups - p.g0);
-  } else {
-    p.g0 = p.cb / g.cparts;
-    const int in = (p.cb % g.cparts) * g.cols;
-    p.vec0 = p.g0 * g.unit_vec + in;
-    p.nvec = min(g.cols, g.unit_vec - in);
-    p.ng = 1;
-  }
-  return p;
-}
-
-__device__ __forceinline__ int64_t site_at(const NormGeom& g, int64_t s,
-                                           int64_t sh, int64_t sw) {
-  if (g.h1) return s * sw;
-  const int64_t y = s / g.w;
-  return y * sh + (s - y * g.w) * sw;
-}
-
-// (na, ma, qa) becomes count, mean and squared deviations of both sets.
-template <typename F>
-__device__ __forceinline__ void merge(F& na, F& ma, F& qa, F nb, F mb, F qb) {
-  if (nb == 0) return;
-  if (na == 0) {
-    na = nb;
-    ma = mb;
-    qa = qb;
-    return;
-  }
-  const F n = na + nb, d = mb - ma, w = nb / n;
-  ma += d * w;
-  qa += qb + d * d * na * w;
-  na = n;
-}
+// sites whose loads a thread has in flight
+constexpr int kBatch = 4, kSumBatch = 8;
 
 // Adds a batch of M values to (cnt, mean, m2): the batch's own mean first,
 // then its squared deviations from that mean.  Values come relative to one
@@ -136,450 +39,328 @@ __device__ __forceinline__ void add_batch(const float* f, float& cnt,
   cnt = n;
 }
 
-// Tree over a block's rows, then over a group's columns.  WHOLE: one entry
-// per thread; otherwise V, one per channel.  Entries of group j end at slot
-// j of out (count, mean, M2).
-template <int V, bool WHOLE>
-__device__ __forceinline__ void block_moments(const NormGeom& g,
-                                              const Place& p, float* cnt,
-                                              float* mean, float* m2,
-                                              float* out) {
-  constexpr int S = WHOLE ? 1 : V;
-  __shared__ float sc[kThreads * S], sm[kThreads * S], sq[kThreads * S];
-  const int tid = threadIdx.x, col = tid % g.cols, row = tid / g.cols;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < S; ++i) {
-    sc[tid * S + i] = cnt[i];
-    sm[tid * S + i] = mean[i];
-    sq[tid * S + i] = m2[i];
-  }
-  __syncthreads();
-  int half = 1;
-  while (half * 2 < g.rows) half *= 2;
-  for (; half >= 1; half >>= 1) {
-    if (row < half && row + half < g.rows) {
-      const int a = tid * S, b = (tid + half * g.cols) * S;
-      for (int i = 0; i < S; ++i)
-        merge(sc[a + i], sm[a + i], sq[a + i], sc[b + i], sm[b + i],
-              sq[b + i]);
-    }
-    __syncthreads();
-  }
-  if constexpr (WHOLE) {
-    const int gw = g.cparts == 1 ? g.unit_vec : p.nvec;  // a group's vectors
-    const int in = col % gw;
-    half = 1;
-    while (half * 2 < gw) half *= 2;
-    for (; half >= 1; half >>= 1) {
-      if (row == 0 && in < half && in + half < gw && col + half < p.nvec)
-        merge(sc[tid], sm[tid], sq[tid], sc[tid + half], sm[tid + half],
-              sq[tid + half]);
-      __syncthreads();
-    }
-    if (tid < p.ng) {
-      out[tid * 3] = sc[tid * gw];
-      out[tid * 3 + 1] = sm[tid * gw];
-      out[tid * 3 + 2] = sq[tid * gw];
-    }
-  } else {
-    // fewer than 32 channels to a group here
-    for (int j = tid; j < p.ng; j += kThreads) {
-      float n = 0.f, m = 0.f, q = 0.f;
-      for (int i = j * g.cpg; i < (j + 1) * g.cpg; ++i)
-        merge(n, m, q, sc[i], sm[i], sq[i]);
-      out[j * 3] = n;
-      out[j * 3 + 1] = m;
-      out[j * 3 + 2] = q;
-    }
-  }
-}
-
 // The value of a group that its values are taken relative to: the first
 // channel of the first site.
 template <typename T>
 __device__ __forceinline__ float base_of(const NormArgs& a, int n, int gr) {
-  return to_f(((const T*)a.x)[n * a.xn + (int64_t)gr * a.g.cpg]);
+  return to_f(((const T*)a.x.p)[n * a.x.sn + (int64_t)gr * a.g.cpg]);
 }
 
-// First pass: count, mean and squared deviations of every site range.
+// The moments of a vector of values, or (not WHOLE) of each of its channels.
+template <int V, bool WHOLE>
+struct Moments {
+  static constexpr int S = WHOLE ? 1 : V;
+  float base[S], cnt[S], mean[S], m2[S];
+  __device__ __forceinline__ Moments() {
+#pragma unroll
+    for (int i = 0; i < S; ++i) base[i] = cnt[i] = mean[i] = m2[i] = 0.f;
+  }
+  template <typename T>
+  __device__ __forceinline__ void set_base(const NormArgs& a, int n, int ch) {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      base[i] = base_of<T>(a, n, (ch + i) / a.g.cpg);
+  }
+  template <typename T, int N>
+  __device__ __forceinline__ void add(const Pack<T, V>* r) {
+    float f[N][V];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      unpack<T, V>(r[k], f[k]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[k][i] -= base[WHOLE ? 0 : i];
+    }
+    if constexpr (WHOLE) {
+      add_batch<N * V>(&f[0][0], cnt[0], mean[0], m2[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float t[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k] = f[k][i];
+        add_batch<N>(t, cnt[i], mean[i], m2[i]);
+      }
+    }
+  }
+};
+
+// Joins the block's moments: group j of the block ends at out[3 j] (count,
+// mean, squared deviations), for all its threads.  Means first, then the
+// deviations from the joint mean, over the lanes that share a group.
+template <int V, bool WHOLE, int TH>
+__device__ __forceinline__ void block_moments(const NormGeom& g,
+                                              const Place& p,
+                                              const Moments<V, WHOLE>& m,
+                                              float* out) {
+  constexpr int S = WHOLE ? 1 : V;
+  __shared__ float sc[TH * S], sm[TH * S], sq[TH * S];
+  const int tid = threadIdx.x;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    sc[tid * S + i] = m.cnt[i];
+    sm[tid * S + i] = m.mean[i];
+    sq[tid * S + i] = m.m2[i];
+  }
+  __syncthreads();
+  const int wide = !WHOLE ? g.cpg : g.cparts == 1 ? g.unit_vec : p.nvec;
+  const int lanes = lanes_per_group(TH, p.ng), in = tid & (lanes - 1);
+  const Entries first(in, lanes, wide);
+  for (int j = tid / lanes; j < p.ng; j += TH / lanes) {
+    float n = 0.f, q = 0.f;
+    double s = 0;   // (its values need not be near zero)
+    for (Entries e = first; e.row < g.rows; e.next()) {
+      const int at = e.row * g.cols * S + j * wide + e.c;
+      n += sc[at];
+      s += (double)sc[at] * sm[at];
+    }
+    n = lanes_sum(n, lanes);
+    const float mean = (float)(lanes_sum(s, lanes) / n);
+    for (Entries e = first; e.row < g.rows; e.next()) {
+      const int at = e.row * g.cols * S + j * wide + e.c;
+      const float d = sm[at] - mean;
+      q += sq[at] + sc[at] * d * d;   // (no values: count and mean are zero)
+    }
+    q = lanes_sum(q, lanes);
+    if (in == 0) {
+      out[j * 3] = n;
+      out[j * 3 + 1] = mean;
+      out[j * 3 + 2] = q;
+    }
+  }
+  __syncthreads();
+}
+
+// Large images, first: the moments of a range of sites.
 template <typename T, int V, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void k_norm_stats(NormArgs a) {
+__device__ __forceinline__ void stats_unit(const NormArgs& a, const Place& p,
+                                           float* res) {
+  const NormGeom& g = a.g;
+  const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
+  Moments<V, WHOLE> m;
+  if (row < g.rows && col < p.nvec) {
+    const int ch = (p.vec0 + col) * V;
+    m.template set_base<T>(a, p.n, ch);
+    int64_t s = p.s0 + row;
+    SiteWalk<const T> x(a.x, p.n, s, ch);
+    Pack<T, V> r[kSumBatch];
+    for (; s + (kSumBatch - 1) * g.rows < p.s1; s += kSumBatch * g.rows) {
+#pragma unroll
+      for (int k = 0; k < kSumBatch; ++k) {
+        r[k] = load_pack<T, V>(x.p);
+        x.next();
+      }
+      m.template add<T, kSumBatch>(r);
+    }
+    for (; s < p.s1; s += g.rows) {
+      r[0] = load_pack<T, V>(x.p);
+      x.next();
+      m.template add<T, 1>(r);
+    }
+  }
+  block_moments<V, WHOLE, kThreads>(g, p, m, res);
+  const int part = p.slab * g.cparts + p.cb % g.cparts;
+  for (int j = threadIdx.x; j < p.ng; j += kThreads) {
+    float* o = a.part +
+               (((int64_t)p.n * g.groups + p.g0 + j) * a.parts + part) * 3;
+    o[0] = res[j * 3];
+    o[1] = res[j * 3 + 1];
+    o[2] = res[j * 3 + 2];
+    // kept: y may take x's place before all blocks have read it there
+    if (part == 0)
+      a.bases[(int64_t)p.n * g.groups + p.g0 + j] =
+          base_of<T>(a, p.n, p.g0 + j);
+  }
+}
+
+// Mean and rstd of the block's groups from their parts: group j at res[2 j],
+// for all threads.
+__device__ __forceinline__ void join_parts(const NormArgs& a, const Place& p,
+                                           float* res) {
+  const NormGeom& g = a.g;
+  const int lanes = lanes_per_group(kThreads, p.ng);
+  const int in = threadIdx.x & (lanes - 1);
+  for (int j = threadIdx.x / lanes; j < p.ng; j += kThreads / lanes) {
+    const int64_t at = (int64_t)p.n * g.groups + p.g0 + j;
+    const float* part = a.part + at * a.parts * 3;
+    float q = 0.f;
+    double n = 0, s = 0;
+#pragma unroll 4
+    for (int i = in; i < a.parts; i += lanes) {
+      n += part[i * 3];
+      s += (double)part[i * 3] * part[i * 3 + 1];
+    }
+    n = lanes_sum(n, lanes);
+    const double md = lanes_sum(s, lanes) / n;
+    const float m = (float)md;
+#pragma unroll 4
+    for (int i = in; i < a.parts; i += lanes) {
+      const float d = part[i * 3 + 1] - m;
+      q += part[i * 3 + 2] + part[i * 3] * d * d;
+    }
+    q = lanes_sum(q, lanes);
+    const float mean = (float)(a.bases[at] + md);
+    const float rstd = 1.f / sqrtf(q / (float)n + a.eps);
+    if (in == 0) {
+      res[j * 2] = mean;
+      res[j * 2 + 1] = rstd;
+      if (a.mean_out && p.slab == 0 && p.cb % g.cparts == 0) {
+        a.mean_out[at] = mean;
+        a.rstd_out[at] = rstd;
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// Normalised, scaled, activated.
+template <typename T, typename O, int V, bool WHOLE, int ACT, bool STREAM>
+__device__ __forceinline__ void put_norm(O* y, const Pack<T, V>& r,
+                                         const Params<V, WHOLE>& q,
+                                         const float* scale) {
+  float f[V];
+  unpack<T, V>(r, f);
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    f[i] = act_fwd<ACT>(
+        __builtin_fmaf(f[i] - q.mu(i), scale[i], q.beta[i]));
+  if constexpr (STREAM)
+    stream_out<O, V>(y, f);
+  else
+    store_pack<O, V>(y, f);
+}
+
+// Large images, then: normalise a range of sites.
+template <typename T, typename O, int V, bool WHOLE, int ACT>
+__device__ __forceinline__ void apply_unit(const NormArgs& a, const Place& p,
+                                           float* res) {
+  const NormGeom& g = a.g;
+  const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
+  join_parts(a, p, res);
+  if (row >= g.rows || col >= p.nvec) return;
+  const int ch = (p.vec0 + col) * V;
+  Params<V, WHOLE> q;
+  q.load_affine(a, ch);
+  q.load_stats(res, 2, ch, g.cpg, p.g0);
+  float scale[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) scale[i] = q.r(i) * q.gamma[i];
+  int64_t s = p.s0 + row;
+  SiteWalk<const T> x(a.x, p.n, s, ch);
+  SiteWalk<O> y(a.y, p.n, s, ch);
+  Pack<T, V> r[kBatch];
+  for (; s + (kBatch - 1) * g.rows < p.s1; s += kBatch * g.rows) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      r[k] = stream_pack<T, V>(x.p);
+      x.next();
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      put_norm<T, O, V, WHOLE, ACT, true>(y.p, r[k], q, scale);
+      y.next();
+    }
+  }
+  for (; s < p.s1; s += g.rows) {
+    put_norm<T, O, V, WHOLE, ACT, true>(y.p, load_pack<T, V>(x.p), q, scale);
+    x.next();
+    y.next();
+  }
+}
+
+// A launch over large images: blocks finish the images [end0, end1) and sum up
+// [sum0, sum1), in turn, so that reads and writes mix.
+template <typename T, typename O, int V, bool WHOLE, int ACT>
+__global__ __launch_bounds__(kThreads) void k_norm_pass(NormArgs a) {
+  __shared__ float res[kMaxCols * (WHOLE ? 1 : V) * 3];
+  const int ends = (a.end1 - a.end0) * a.g.units;
+  const int all = ends + (a.sum1 - a.sum0) * a.g.units;
+  for (int b = blockIdx.x; b < all; b += gridDim.x) {
+    const Turn t(a, b, ends, all);
+    const Place p = place_of(a.g, t.n, t.u);
+    if (t.end)
+      apply_unit<T, O, V, WHOLE, ACT>(a, p, res);
+    else
+      stats_unit<T, V, WHOLE>(a, p, res);
+    __syncthreads();
+  }
+}
+
+// Images whose groups fit a block's registers: one launch, x read once.  A
+// thread holds up to kHeld sites of its vector.
+template <typename T, typename O, int V, bool WHOLE, int TH>
+__global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
   constexpr int S = WHOLE ? 1 : V;
   const NormGeom& g = a.g;
-  __shared__ float res[kThreads * 8 * 3];
+  __shared__ float res[kMaxCols * S * 3];
   const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  for (int64_t u = blockIdx.x; u < g.units; u += gridDim.x) {
-    const Place p = place_of(g, u);
-    float cnt[S], mean[S], m2[S], base[S];
+  const int u = near_block(g.n * g.units);
+  const Place p = place_of(g, u / g.units, u % g.units);
+  const bool on = row < g.rows && col < p.nvec;
+  const int ch = (p.vec0 + (on ? col : 0)) * V;
+  const int left = on ? (int)g.sites - row : 0;   // sites from its own on
+  Pack<T, V> r[kHeld];
+  SiteWalk<const T> x(a.x, p.n, row, ch);
 #pragma unroll
-    for (int i = 0; i < S; ++i) cnt[i] = mean[i] = m2[i] = 0.f;
-    if (row < g.rows && col < p.nvec) {
-      const int ch = (p.vec0 + col) * V;
-#pragma unroll
-      for (int i = 0; i < S; ++i) base[i] = base_of<T>(a, p.n, (ch + i) / g.cpg);
-      const T* x = (const T*)a.x + p.n * a.xn + ch;
-      int64_t s = p.s0 + row;
-      for (; s + (kBatch - 1) * g.rows < p.s1; s += kBatch * g.rows) {
-        Pack<T, V> r[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-          r[k] = load_pack<T, V>(
-              x + site_at(g, s + k * g.rows, a.xh, a.xw));
-        float f[kBatch][V];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-          unpack<T, V>(r[k], f[k]);
-#pragma unroll
-          for (int i = 0; i < V; ++i) f[k][i] -= base[WHOLE ? 0 : i];
-        }
-        if constexpr (WHOLE) {
-          add_batch<kBatch * V>(&f[0][0], cnt[0], mean[0], m2[0]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float t[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) t[k] = f[k][i];
-            add_batch<kBatch>(t, cnt[i], mean[i], m2[i]);
-          }
-        }
-      }
-      for (; s < p.s1; s += g.rows) {
-        float f[V];
-        unpack<T, V>(load_pack<T, V>(x + site_at(g, s, a.xh, a.xw)), f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] -= base[WHOLE ? 0 : i];
-        if constexpr (WHOLE) {
-          add_batch<V>(f, cnt[0], mean[0], m2[0]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i)
-            add_batch<1>(f + i, cnt[i], mean[i], m2[i]);
-        }
-      }
-    }
-    block_moments<V, WHOLE>(g, p, cnt, mean, m2, res);
-    __syncthreads();
-    const int part = p.slab * g.cparts + p.cb % g.cparts;
-    for (int j = threadIdx.x; j < p.ng; j += kThreads) {
-      float* o = a.part +
-                 (((int64_t)p.n * g.groups + p.g0 + j) * a.parts + part) * 3;
-      o[0] = res[j * 3];
-      o[1] = res[j * 3 + 1];
-      o[2] = res[j * 3 + 2];
-    }
-    __syncthreads();
+  for (int k = 0; k < kHeld; ++k) {
+    if (k * g.rows < left) r[k] = load_pack<T, V>(x.p);
+    x.next();
   }
-}
-
-// Mean and rstd of one image and group from its parts, by one wave, in f64
-// (every lane ends with them).
-template <typename T>
-__device__ __forceinline__ void join_parts(const NormArgs& a, int64_t ng,
-                                           float& mean, float& rstd) {
-  const float* part = a.part + ng * a.parts * 3;
-  const int lane = threadIdx.x & 63;
-  double n = 0, m = 0, q = 0;
-  for (int i = lane; i < a.parts; i += 64)
-    merge<double>(n, m, q, part[i * 3], part[i * 3 + 1], part[i * 3 + 2]);
-  for (int d = 32; d; d >>= 1) {
-    const double on = __shfl_down(n, d), om = __shfl_down(m, d),
-                 oq = __shfl_down(q, d);
-    if (lane + d < 64) merge(n, m, q, on, om, oq);
-  }
-  const double base =
-      base_of<T>(a, (int)(ng / a.g.groups), (int)(ng % a.g.groups));
-  mean = (float)(base + __shfl(m, 0));
-  rstd = (float)__shfl(1.0 / sqrt(q / n + (double)a.eps), 0);
-}
-
-// One wave per image and group.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_join(NormArgs a) {
-  const int64_t total = (int64_t)a.g.n * a.g.groups;
-  for (int64_t i = blockIdx.x * 4ll + threadIdx.x / 64; i < total;
-       i += gridDim.x * 4ll) {
-    float m, r;
-    join_parts<T>(a, i, m, r);
-    if ((threadIdx.x & 63) == 0) {
-      a.mean_out[i] = m;
-      a.rstd_out[i] = r;
+  Moments<V, WHOLE> m;
+  m.template set_base<T>(a, p.n, ch);
+  Params<V, WHOLE> q;
+  q.load_affine(a, ch);
+  const float jbase = base_of<T>(a, p.n, min(p.g0 + (int)threadIdx.x,
+                                             g.groups - 1));
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (k * g.rows < left) m.template add<T, 1>(r + k);
+  block_moments<V, WHOLE, TH>(g, p, m, res);
+  for (int j = threadIdx.x; j < p.ng; j += TH) {
+    const float mean =
+        (j < TH ? jbase : base_of<T>(a, p.n, p.g0 + j)) + res[j * 3 + 1];
+    const float rstd = 1.f / sqrtf(res[j * 3 + 2] / res[j * 3] + a.eps);
+    res[j * 3] = mean;
+    res[j * 3 + 1] = rstd;
+    if (a.mean_out) {
+      const int64_t at = (int64_t)p.n * g.groups + p.g0 + j;
+      a.mean_out[at] = mean;
+      a.rstd_out[at] = rstd;
     }
   }
-}
-
-// A thread's channels: mean and rstd * gamma, beta.
-template <int V>
-__device__ __forceinline__ void load_params(const NormArgs& a, int n, int ch,
-                                            float* mean, float* rstd,
-                                            float* gamma, float* beta) {
+  __syncthreads();
+  float scale[V];
+  q.load_stats(res, 3, ch, g.cpg, p.g0);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int64_t at = (int64_t)n * a.g.groups + (ch + i) / a.g.cpg;
-    mean[i] = a.mean[at];
-    rstd[i] = a.rstd[at];
-    gamma[i] = a.gamma ? a.gamma[ch + i] : 1.f;
-    beta[i] = a.beta ? a.beta[ch + i] : 0.f;
-  }
-}
-
-// Last pass: normalise, activate.
-template <typename T, typename O, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_apply(NormArgs a) {
-  const NormGeom& g = a.g;
-  const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  for (int64_t u = blockIdx.x; u < g.units; u += gridDim.x) {
-    const Place p = place_of(g, u);
-    if (row >= g.rows || col >= p.nvec) continue;
-    const int ch = (p.vec0 + col) * V;
-    float mean[V], scale[V], gamma[V], beta[V];
-    load_params<V>(a, p.n, ch, mean, scale, gamma, beta);
+  for (int i = 0; i < V; ++i) scale[i] = q.r(i) * q.gamma[i];
+  SiteWalk<O> y(a.y, p.n, row, ch);
+  with_activation_of(a.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) scale[i] *= gamma[i];
-    const T* x = (const T*)a.x + p.n * a.xn + ch;
-    O* y = (O*)a.y + p.n * a.yn + ch;
-    auto put = [&](int64_t s, const Pack<T, V>& r) {
-      float f[V];
-      unpack<T, V>(r, f);
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        f[i] = act_fwd<ACT>(
-            __builtin_fmaf(f[i] - mean[i], scale[i], beta[i]));
-      store_pack<O, V>(y + site_at(g, s, a.yh, a.yw), f);
-    };
-    int64_t s = p.s0 + row;
-    for (; s + (kBatch - 1) * g.rows < p.s1; s += kBatch * g.rows) {
-      Pack<T, V> r[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k)
-        r[k] = load_pack<T, V>(x + site_at(g, s + k * g.rows, a.xh, a.xw));
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) put(s + k * g.rows, r[k]);
+    for (int k = 0; k < kHeld; ++k) {
+      if (k * g.rows < left)
+        put_norm<T, O, V, WHOLE, decltype(act)::value, false>(y.p, r[k], q,
+                                                              scale);
+      y.next();
     }
-    for (; s < p.s1; s += g.rows)
-      put(s, load_pack<T, V>(x + site_at(g, s, a.xh, a.xw)));
-  }
-}
-
-// ---------------------------------------------------------------- backward
-
-// dz and xh of one vector.
-template <int V, int ACT>
-__device__ __forceinline__ void dz_of(const float* x, float* dy,
-                                      const float* mean, const float* rstd,
-                                      const float* gamma, const float* beta,
-                                      float* xh) {
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    xh[i] = (x[i] - mean[i]) * rstd[i];
-    if constexpr (ACT != ST_ACT_NONE)
-      dy[i] *= act_grad<ACT>(__builtin_fmaf(xh[i], gamma[i], beta[i]));
-  }
-}
-
-// First pass: sums of dz and dz xh per channel and site range.
-template <typename T, typename O, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_grad_sums(NormArgs a) {
-  const NormGeom& g = a.g;
-  __shared__ float red[kThreads * V * 2];
-  const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  for (int64_t u = blockIdx.x; u < g.units; u += gridDim.x) {
-    const Place p = place_of(g, u);
-    float s1[V], s2[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.f;
-    const int ch = (p.vec0 + col) * V;
-    if (row < g.rows && col < p.nvec) {
-      float mean[V], rstd[V], gamma[V], beta[V];
-      load_params<V>(a, p.n, ch, mean, rstd, gamma, beta);
-      const T* x = (const T*)a.x + p.n * a.xn + ch;
-      const O* dy = (const O*)a.dy + p.n * a.dn + ch;
-      auto add = [&](const Pack<T, V>& rx, const Pack<O, V>& rd) {
-        float f[V], d[V], xh[V];
-        unpack<T, V>(rx, f);
-        unpack<O, V>(rd, d);
-        dz_of<V, ACT>(f, d, mean, rstd, gamma, beta, xh);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          s1[i] += d[i];
-          s2[i] = __builtin_fmaf(d[i], xh[i], s2[i]);
-        }
-      };
-      int64_t s = p.s0 + row;
-      for (; s + (kBatch - 1) * g.rows < p.s1; s += kBatch * g.rows) {
-        Pack<T, V> rx[kBatch];
-        Pack<O, V> rd[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-          rx[k] = load_pack<T, V>(x + site_at(g, s + k * g.rows, a.xh, a.xw));
-          rd[k] = load_pack<O, V>(dy +
-                                  site_at(g, s + k * g.rows, a.dh, a.dw));
-        }
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) add(rx[k], rd[k]);
-      }
-      for (; s < p.s1; s += g.rows)
-        add(load_pack<T, V>(x + site_at(g, s, a.xh, a.xw)),
-            load_pack<O, V>(dy + site_at(g, s, a.dh, a.dw)));
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      red[(threadIdx.x * V + i) * 2] = s1[i];
-      red[(threadIdx.x * V + i) * 2 + 1] = s2[i];
-    }
-    __syncthreads();
-    int half = 1;
-    while (half * 2 < g.rows) half *= 2;
-    for (; half >= 1; half >>= 1) {
-      if (row < half && row + half < g.rows) {
-        const int x0 = threadIdx.x * V * 2, x1 = x0 + half * g.cols * V * 2;
-        for (int i = 0; i < 2 * V; ++i) red[x0 + i] += red[x1 + i];
-      }
-      __syncthreads();
-    }
-    float* o = a.part + ((int64_t)p.n * g.slabs + p.slab) * g.c * 2 +
-               (int64_t)p.vec0 * V * 2;
-    for (int i = threadIdx.x; i < p.nvec * V * 2; i += kThreads) o[i] = red[i];
-  }
-}
-
-// One block per image and group: sums over the site ranges, per channel
-// (kept for dgamma and dbeta) and, weighted, over the group.
-__global__ __launch_bounds__(kThreads) void k_norm_grad_join(NormArgs a) {
-  const NormGeom& g = a.g;
-  __shared__ double r1[kThreads], r2[kThreads];
-  const int64_t total = (int64_t)g.n * g.groups;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    const int n = (int)(u / g.groups), gr = (int)(u % g.groups);
-    // threads of a channel take its site ranges in turn
-    int per = 1;
-    while (per * 2 * g.cpg <= kThreads && per < g.slabs) per *= 2;
-    const int chs = kThreads / per;
-    double t1 = 0, t2 = 0;
-    for (int c0 = 0; c0 < g.cpg; c0 += chs) {
-      const int c = c0 + threadIdx.x % chs, k = threadIdx.x / chs;
-      double d1 = 0, d2 = 0;
-      if (c < g.cpg) {
-        const float* p =
-            a.part + ((int64_t)n * g.slabs * g.c + gr * g.cpg + c) * 2;
-        for (int s = k; s < g.slabs; s += per) {
-          d1 += p[(int64_t)s * g.c * 2];
-          d2 += p[(int64_t)s * g.c * 2 + 1];
-        }
-      }
-      __syncthreads();
-      r1[threadIdx.x] = d1;
-      r2[threadIdx.x] = d2;
-      __syncthreads();
-      if (k == 0 && c < g.cpg) {
-        for (int s = 1; s < per; ++s) {
-          d1 += r1[s * chs + threadIdx.x];
-          d2 += r2[s * chs + threadIdx.x];
-        }
-        float* o = a.chsum + ((int64_t)n * g.c + gr * g.cpg + c) * 2;
-        o[0] = (float)d1;
-        o[1] = (float)d2;
-        const double gm = a.gamma ? a.gamma[gr * g.cpg + c] : 1.f;
-        t1 += d1 * gm;
-        t2 += d2 * gm;
-      }
-    }
-    __syncthreads();
-    r1[threadIdx.x] = t1;
-    r2[threadIdx.x] = t2;
-    __syncthreads();
-    for (int d = kThreads / 2; d; d >>= 1) {
-      if ((int)threadIdx.x < d) {
-        r1[threadIdx.x] += r1[threadIdx.x + d];
-        r2[threadIdx.x] += r2[threadIdx.x + d];
-      }
-      __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-      const double m = (double)g.sites * g.cpg;
-      a.gsum[u * 2] = (float)(r1[0] / m);
-      a.gsum[u * 2 + 1] = (float)(r2[0] / m);
-    }
-    __syncthreads();
-  }
-}
-
-// Last pass: dx; the first `dblocks` blocks sum dgamma and dbeta over the
-// images.
-template <typename T, typename O, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_grad_apply(NormArgs a) {
-  const NormGeom& g = a.g;
-  if ((int)blockIdx.x < a.dblocks) {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= g.c) return;
-    double d1 = 0, d2 = 0;
-    for (int n = 0; n < g.n; ++n) {
-      d1 += a.chsum[((int64_t)n * g.c + c) * 2];
-      d2 += a.chsum[((int64_t)n * g.c + c) * 2 + 1];
-    }
-    if (a.dbeta) a.dbeta[c] = (float)d1;
-    if (a.dgamma) a.dgamma[c] = (float)d2;
-    return;
-  }
-  const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  for (int64_t u = blockIdx.x - a.dblocks; u < g.units;
-       u += gridDim.x - a.dblocks) {
-    const Place p = place_of(g, u);
-    if (row >= g.rows || col >= p.nvec) continue;
-    const int ch = (p.vec0 + col) * V;
-    float mean[V], rstd[V], gamma[V], beta[V], s1[V], s2[V];
-    load_params<V>(a, p.n, ch, mean, rstd, gamma, beta);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int64_t at = (int64_t)p.n * g.groups + (ch + i) / g.cpg;
-      s1[i] = a.gsum[at * 2];
-      s2[i] = a.gsum[at * 2 + 1];
-    }
-    const T* x = (const T*)a.x + p.n * a.xn + ch;
-    const O* dy = (const O*)a.dy + p.n * a.dn + ch;
-    T* dx = (T*)a.y + p.n * a.yn + ch;
-    auto put = [&](int64_t s, const Pack<T, V>& rx, const Pack<O, V>& rd) {
-      float f[V], d[V], xh[V];
-      unpack<T, V>(rx, f);
-      unpack<O, V>(rd, d);
-      dz_of<V, ACT>(f, d, mean, rstd, gamma, beta, xh);
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        f[i] = rstd[i] * (__builtin_fmaf(d[i], gamma[i], -s1[i]) -
-                          xh[i] * s2[i]);
-      store_pack<T, V>(dx + site_at(g, s, a.yh, a.yw), f);
-    };
-    int64_t s = p.s0 + row;
-    for (; s + (kBatch - 1) * g.rows < p.s1; s += kBatch * g.rows) {
-      Pack<T, V> rx[kBatch];
-      Pack<O, V> rd[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        rx[k] = load_pack<T, V>(x + site_at(g, s + k * g.rows, a.xh, a.xw));
-        rd[k] = load_pack<O, V>(dy + site_at(g, s + k * g.rows, a.dh, a.dw));
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) put(s + k * g.rows, rx[k], rd[k]);
-    }
-    for (; s < p.s1; s += g.rows)
-      put(s, load_pack<T, V>(x + site_at(g, s, a.xh, a.xw)),
-          load_pack<O, V>(dy + site_at(g, s, a.dh, a.dw)));
-  }
+  });
 }
 
 // -------------------------------------------------------------- host side
 
-constexpr int kTargetBlocks = 2048;   // eight of 256 threads to a CU
-constexpr int kMaxSlabs = 1024;
-constexpr int kMinBatches = 2;        // batches a thread has at least
+constexpr int kHeldBlocks = 256;      // one to a CU
+
+constexpr int kTargetBlocks = 1024;   // four of 256 threads to a CU
+constexpr int kMaxEntries = 4096;     // parts of all groups a block joins
+constexpr int kMinSites = 16;         // sites a thread has at least
+constexpr int kLine = 256;            // bytes of a site to a block
+// Bytes of the images of a batch: what is read again after one more batch
+// was read and one written must be in the last-level cache still (256 MiB).
+constexpr int64_t kBatchBytes = 144 << 20;
 
 // The cut for vectors of v channels; false where v does not suit the groups.
 bool geom(const st_norm_desc& d, int v, NormGeom& g) {
   g = NormGeom{};
   g.sites = (int64_t)d.h * d.w;
-  g.w = d.w;
   g.n = d.n;
   g.c = d.c;
   g.groups = d.groups;
@@ -589,40 +370,93 @@ bool geom(const st_norm_desc& d, int v, NormGeom& g) {
   g.cv = d.c / v;
   g.whole = g.cpg % v == 0;
   // vectors that straddle groups: only where groups are narrow, so that a
-  // group's channels are few to join
-  if (!g.whole && g.cpg >= 32) return false;
-  const int mul = v / std::gcd(g.cpg, v);   // groups that fill whole vectors
-  g.unit_vec = g.cpg * mul / v;
-  if (g.unit_vec <= kThreads) {
-    const int units = g.groups / mul;
-    const int fit = std::min(units, kThreads / g.unit_vec);
-    g.colblocks = (int)ceil_div(units, fit);
-    const int per = (int)ceil_div(units, g.colblocks);
-    g.colblocks = (int)ceil_div(units, per);
+  // group's channels are few to join, and the vectors' own sums too
+  if (!g.whole && (g.cpg >= 32 || v > 4)) return false;
+  return true;
+}
+
+// Columns for blocks of `threads`, `units` units of the fewest groups that
+// fill whole vectors in each.
+void columns(NormGeom& g, int threads, int units) {
+  const int mul = g.v / std::gcd(g.cpg, g.v);
+  g.threads = threads;
+  g.unit_vec = g.cpg * mul / g.v;
+  if (g.unit_vec <= kMaxCols) {
+    const int all = g.groups / mul;
+    g.colblocks = (int)ceil_div(all, units);
+    const int per = (int)ceil_div(all, g.colblocks);
+    g.colblocks = (int)ceil_div(all, per);
     g.cols = per * g.unit_vec;
     g.kg = per * mul;
     g.cparts = 1;
   } else {
-    g.cparts = (int)ceil_div(g.unit_vec, kThreads);
+    g.cparts = (int)ceil_div(g.unit_vec, kMaxCols);
     g.cols = (int)ceil_div(g.unit_vec, g.cparts);
     g.cparts = (int)ceil_div(g.unit_vec, g.cols);
     g.colblocks = g.groups * g.cparts;
     g.kg = 1;
   }
-  g.rows = kThreads / g.cols;
-  const int64_t blocks = (int64_t)g.n * g.colblocks;
-  const int64_t most =
-      ceil_div(g.sites, (int64_t)g.rows * kBatch * kMinBatches);
-  int64_t slabs = std::min<int64_t>(most, ceil_div(kTargetBlocks, blocks));
-  slabs = std::max<int64_t>(1, std::min<int64_t>(slabs, kMaxSlabs));
-  g.slab_sites = ceil_div(g.sites, slabs);
-  g.slabs = (int)ceil_div(g.sites, g.slab_sites);
-  g.units = blocks * g.slabs;
+  g.rows = threads / g.cols;
+}
+
+// Blocks that hold an image's groups whole, `held` sites a thread at most.
+bool hold(NormGeom& g, int threads, int held) {
+  const int mul = g.v / std::gcd(g.cpg, g.v);
+  const int unit = g.cpg * mul / g.v;
+  if (unit > kMaxCols) return false;
+  columns(g, threads, 1);
+  if (ceil_div(g.sites, g.rows) > held ||
+      (int64_t)g.n * g.colblocks > kMaxGrid)
+    return false;
+  // wider blocks while there are more than enough: whole cache lines, fewer
+  // of them
+  NormGeom w = g;
+  for (int u = 2; u * unit <= kMaxCols; u *= 2) {
+    columns(w, threads, u);
+    if (ceil_div(w.sites, w.rows) > held ||
+        (int64_t)w.n * w.colblocks < kHeldBlocks)
+      break;
+    g = w;
+  }
+  g.slabs = 1;
+  g.slab_sites = g.sites;
+  g.units = g.colblocks;
   return true;
 }
 
+// Images of a batch, `es` bytes of each element read by both passes.
+int batch_of(const NormGeom& g, int es) {
+  return (int)std::max<int64_t>(
+      1, std::min<int64_t>(g.n, kBatchBytes / (g.sites * g.c * es)));
+}
+
+// Blocks that take a range of an image's sites: columns of at least kLine
+// bytes, and no more ranges than a block of the next pass can join.
+void split(NormGeom& g, int es, int batch) {
+  const int mul = g.v / std::gcd(g.cpg, g.v);
+  const int unit = g.cpg * mul / g.v;
+  columns(g, kThreads, std::max(1, std::min<int>(kMaxCols / unit,
+                        (int)ceil_div(kLine, (int64_t)unit * g.v * es))));
+  const int64_t blocks = (int64_t)batch * g.colblocks;
+  const int64_t most =
+      ceil_div(g.sites, (int64_t)g.rows * kMinSites);
+  int64_t slabs = std::min<int64_t>(most, ceil_div(kTargetBlocks, blocks));
+  slabs = std::min<int64_t>(slabs, kMaxEntries / (g.kg * g.cparts));
+  slabs = std::max<int64_t>(1, slabs);
+  g.slab_sites = ceil_div(g.sites, slabs);
+  g.slabs = (int)ceil_div(g.sites, g.slab_sites);
+  g.units = g.slabs * g.colblocks;
+}
+
+int read_size(const st_norm_desc& d, bool backward) {
+  return esize(d.dtype) + (backward ? esize(d.out_dtype) : 0);
+}
+void split_for(const st_norm_desc& d, NormGeom& g, bool backward) {
+  split(g, esize(d.dtype), batch_of(g, read_size(d, backward)));
+}
+
 struct NormSpace {
-  size_t part = 0, chsum = 0, gsum = 0, stats = 0, bytes = 0;
+  size_t part = 0, bases = 0, chpart = 0, bytes = 0;
 };
 NormSpace space_of(const NormGeom& g, bool backward) {
   NormSpace s;
@@ -632,15 +466,12 @@ NormSpace space_of(const NormGeom& g, bool backward) {
     top += (size_t)round_up(floats * 4, (int64_t)kAlign);
     return at;
   };
-  const int64_t ng = (int64_t)g.n * g.groups;
-  if (backward) {
-    s.part = take((int64_t)g.n * g.slabs * g.c * 2);
-    s.chsum = take((int64_t)g.n * g.c * 2);
-    s.gsum = take(ng * 2);
-  } else {
-    s.part = take(ng * g.slabs * g.cparts * 3);
-    s.stats = take(ng * 2);
-  }
+  s.part = take((int64_t)g.n * g.groups * g.slabs * g.cparts *
+                (backward ? 2 : 3));
+  if (backward)
+    s.chpart = take((int64_t)g.n * g.slabs * g.c * 2);
+  else
+    s.bases = take((int64_t)g.n * g.groups);
   s.bytes = top;
   return s;
 }
@@ -651,6 +482,8 @@ st_status check_desc(const st_norm_desc* d) {
     return bad("unknown data types, or a pair that is not offered");
   if (d->n < 0 || d->h < 1 || d->w < 1 || d->c < 1)
     return bad("the map's sizes must be positive (n may be 0)");
+  if ((int64_t)d->n * d->c >= (int64_t)1 << 31)
+    return bad("n * c must lie below 2^31");
   if (d->groups < 1 || d->c % d->groups)
     return bad("groups must divide the channels");
   if (!act_known(d->act)) return bad("unknown activation");
@@ -714,29 +547,34 @@ NormGeom pick(const st_norm_desc& d, std::initializer_list<MapUse> maps) {
     if (ok && geom(d, v, g)) break;
   }
   if (v == 1) (void)geom(d, 1, g);
-  g.h1 = 1;
-  for (const MapUse& u : maps)
-    if (d.h > 1 && d.w > 1 && u.m->stride_h != u.m->stride_w * d.w) g.h1 = 0;
   return g;
 }
-// A map of one column steps by rows.
-int64_t step_w(const st_norm_desc& d, const st_map_ref& m) {
-  return d.w == 1 ? m.stride_h : m.stride_w;
+// A map for blocks of g.rows sites at a time.
+NormMap map_of(const st_norm_desc& d, const st_map_ref& m,
+               const NormGeom& g) {
+  NormMap r{m.data, m.stride_n, m.stride_h, m.stride_w, d.w, 0, 0, 0};
+  if (d.h == 1 || d.w == 1 || m.stride_h == m.stride_w * d.w) {
+    // evenly apart: a line to each site
+    r.sh = d.w == 1 ? m.stride_h : m.stride_w;
+    r.w = 1;
+    r.step = g.rows * r.sh;
+    return r;
+  }
+  r.dx = g.rows % d.w;
+  r.step = g.rows / d.w * r.sh + r.dx * r.sw;
+  r.wrap = r.sh - d.w * r.sw;
+  return r;
 }
-
-template <class F>
-void with_vec(int v, F&& f) {
-  if (v == 8)
-    f(Int<8>{});
-  else if (v == 4)
-    f(Int<4>{});
-  else if (v == 2)
-    f(Int<2>{});
-  else
-    f(Int<1>{});
-}
-unsigned grid_of(int64_t units) {
-  return (unsigned)std::min<int64_t>(units, 1 << 20);
+// The threads of the blocks that hold the image's groups (of x and dy in the
+// backward pass), or 0 and a cut into site ranges.  (A block that holds up to
+// 128 KiB takes about as long as a second launch would; larger groups go over
+// all CUs in ranges.)
+int hold_or_split(const st_norm_desc& d, NormGeom& g, bool backward) {
+  if (hold(g, kFewThreads, kHeld)) return kFewThreads;
+  if (hold(g, kManyThreads, backward ? kHeld / 2 : kHeld))
+    return kManyThreads;
+  split_for(d, g, backward);
+  return 0;
 }
 
 st_status workspace_of(const st_norm_desc* d, int32_t backward,
@@ -747,8 +585,9 @@ st_status workspace_of(const st_norm_desc* d, int32_t backward,
   *bytes = 0;
   for (int v = 8; v >= 1 && d->n > 0; v /= 2) {
     NormGeom g;
-    if (geom(*d, v, g))
-      *bytes = std::max<uint64_t>(*bytes, space_of(g, backward != 0).bytes);
+    if (!geom(*d, v, g)) continue;
+    split_for(*d, g, backward != 0);
+    *bytes = std::max<uint64_t>(*bytes, space_of(g, backward != 0).bytes);
   }
   return ST_OK;
 }
@@ -766,6 +605,30 @@ st_status check_space(const st_norm_desc& d, bool backward, const void* ws,
 }
 
 }  // namespace
+
+void launch_norm(const NormArgs& a, int dtype, int out_dtype, int held,
+                 int batch, hipStream_t q) {
+  const unsigned grid = (unsigned)((int64_t)a.g.n * a.g.units);
+  with_norm(dtype, out_dtype, a.g, [&](auto ti, auto to, auto vt, auto wt) {
+    using T = typename decltype(ti)::type;
+    using O = typename decltype(to)::type;
+    constexpr int V = decltype(vt)::value;
+    constexpr bool W = decltype(wt)::value;
+    if (held == kFewThreads) {
+      k_norm_held<T, O, V, W, kFewThreads><<<grid, kFewThreads, 0, q>>>(a);
+    } else if (held == kManyThreads) {
+      k_norm_held<T, O, V, W, kManyThreads><<<grid, kManyThreads, 0, q>>>(a);
+    } else {
+      with_activation(a.act, [&](auto act) {
+        with_batches(a, batch, [&](const NormArgs& b, bool) {
+          k_norm_pass<T, O, V, W, decltype(act)::value>
+              <<<pass_blocks(b), kThreads, 0, q>>>(b);
+        });
+      });
+    }
+  });
+}
+
 }  // namespace ops
 }  // namespace st
 
@@ -808,46 +671,22 @@ extern "C" st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
     (void)hipGetLastError();
     NormArgs a{};
     a.g = pick(*d, {{x, es}, {y, eo}});
+    const int held = hold_or_split(*d, a.g, false);
+    a.act = d->act;
     const NormSpace sp = space_of(a.g, false);
     char* w = (char*)ws;
-    a.x = x->data;
-    a.y = y->data;
-    a.xn = x->stride_n; a.xh = x->stride_h; a.xw = step_w(*d, *x);
-    a.yn = y->stride_n; a.yh = y->stride_h; a.yw = step_w(*d, *y);
+    a.x = map_of(*d, *x, a.g);
+    a.y = map_of(*d, *y, a.g);
     a.gamma = gamma;
     a.beta = beta;
     a.eps = d->eps;
     a.part = (float*)(w + sp.part);
+    a.bases = (float*)(w + sp.bases);
     a.parts = a.g.slabs * a.g.cparts;
-    a.mean_out = mean ? mean : (float*)(w + sp.stats);
-    a.rstd_out = rstd ? rstd : a.mean_out + (int64_t)d->n * d->groups;
-    a.mean = a.mean_out;
-    a.rstd = a.rstd_out;
-    hipStream_t q = (hipStream_t)stream;
-    with_types(d->dtype, d->out_dtype, [&](auto in, auto out) {
-      using T = typename decltype(in)::type;
-      using O = typename decltype(out)::type;
-      with_vec(a.g.v, [&](auto vt) {
-        constexpr int V = decltype(vt)::value;
-        if constexpr (V * sizeof(T) <= 16 && V * sizeof(O) <= 16) {
-          if constexpr (V == 1)
-            k_norm_stats<T, 1, true>
-                <<<grid_of(a.g.units), kThreads, 0, q>>>(a);
-          else if (a.g.whole)
-            k_norm_stats<T, V, true>
-                <<<grid_of(a.g.units), kThreads, 0, q>>>(a);
-          else
-            k_norm_stats<T, V, false>
-                <<<grid_of(a.g.units), kThreads, 0, q>>>(a);
-          k_norm_join<T><<<grid_of(ceil_div((int64_t)d->n * d->groups, 4)),
-                           kThreads, 0, q>>>(a);
-          with_activation(d->act, [&](auto act) {
-            k_norm_apply<T, O, V, decltype(act)::value>
-                <<<grid_of(a.g.units), kThreads, 0, q>>>(a);
-          });
-        }
-      });
-    });
+    a.mean_out = mean;
+    a.rstd_out = rstd;
+    launch_norm(a, d->dtype, d->out_dtype, held,
+                batch_of(a.g, read_size(*d, false)), (hipStream_t)stream);
     return launch_status("group norm");
   });
 }
@@ -863,16 +702,15 @@ extern "C" st_status st_group_norm_backward(
     NormArgs a{};
     a.dgamma = dgamma;
     a.dbeta = dbeta;
+    a.act = d->act;
     a.g.c = d->c;
-    const int dblocks =
-        dgamma || dbeta ? (int)ceil_div(d->c, kThreads) : 0;
+    const int dblocks = dgamma || dbeta ? (int)ceil_div(d->c, 32) : 0;
     if (d->n == 0) {
       // no image: the parameters' gradients are zero
       if (dblocks) {
         (void)hipGetLastError();
         a.dblocks = dblocks;
-        k_norm_grad_apply<float, float, 1, ST_ACT_NONE>
-            <<<dblocks, kThreads, 0, q>>>(a);
+        launch_norm_backward(a, ST_F32, ST_F32, 0, 1, q);
         return launch_status("group norm backward");
       }
       return ST_OK;
@@ -907,41 +745,23 @@ extern "C" st_status st_group_norm_backward(
                  "workspace");
     (void)hipGetLastError();
     a.g = pick(*d, {{x, es}, {dy, eo}, {dx, es}});
+    const int held = hold_or_split(*d, a.g, true);
     const NormSpace sp = space_of(a.g, true);
     char* w = (char*)ws;
-    a.x = x->data;
-    a.dy = dy->data;
-    a.y = dx->data;
-    a.xn = x->stride_n; a.xh = x->stride_h; a.xw = step_w(*d, *x);
-    a.dn = dy->stride_n; a.dh = dy->stride_h; a.dw = step_w(*d, *dy);
-    a.yn = dx->stride_n; a.yh = dx->stride_h; a.yw = step_w(*d, *dx);
+    a.x = map_of(*d, *x, a.g);
+    a.dy = map_of(*d, *dy, a.g);
+    a.y = map_of(*d, *dx, a.g);
     a.gamma = gamma;
     a.beta = beta;
     a.mean = mean;
     a.rstd = rstd;
     a.eps = d->eps;
     a.part = (float*)(w + sp.part);
-    a.chsum = (float*)(w + sp.chsum);
-    a.gsum = (float*)(w + sp.gsum);
+    a.parts = a.g.slabs * a.g.cparts;
+    a.chpart = (float*)(w + sp.chpart);
     a.dblocks = dblocks;
-    with_types(d->dtype, d->out_dtype, [&](auto ti, auto to) {
-      using T = typename decltype(ti)::type;
-      using O = typename decltype(to)::type;
-      with_vec(a.g.v, [&](auto vt) {
-        constexpr int V = decltype(vt)::value;
-        if constexpr (V * sizeof(T) <= 16 && V * sizeof(O) <= 16) {
-          with_activation(d->act, [&](auto act) {
-            constexpr int A = decltype(act)::value;
-            k_norm_grad_sums<T, O, V, A>
-                <<<grid_of(a.g.units), kThreads, 0, q>>>(a);
-            k_norm_grad_join<<<grid_of((int64_t)d->n * d->groups), kThreads,
-                               0, q>>>(a);
-            k_norm_grad_apply<T, O, V, A>
-                <<<grid_of(a.g.units) + dblocks, kThreads, 0, q>>>(a);
-          });
-        }
-      });
-    });
+    launch_norm_backward(a, d->dtype, d->out_dtype, held,
+                         batch_of(a.g, read_size(*d, true)), q);
     return launch_status("group norm backward");
   });
 }

@@ -28,6 +28,32 @@ template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
   return *(const Pack<T, V>*)p;
 }
+// The same past the caches' reuse order: for data that is streamed through
+// once.  Whole lines only (a store of part of one costs a read of the rest).
+template <int N> struct Bits;
+template <> struct Bits<1> { typedef uint8_t type; };
+template <> struct Bits<2> { typedef uint16_t type; };
+template <> struct Bits<4> { typedef uint32_t type; };
+template <> struct Bits<8> {
+  typedef uint32_t type __attribute__((ext_vector_type(2)));
+};
+template <> struct Bits<16> {
+  typedef uint32_t type __attribute__((ext_vector_type(4)));
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> stream_pack(const T* p) {
+  typedef typename Bits<sizeof(T) * V>::type B;
+  const B b = __builtin_nontemporal_load((const B*)p);
+  return __builtin_bit_cast(Pack<T, V>, b);
+}
+template <typename T, int V>
+__device__ __forceinline__ void stream_out(T* p, const float* f) {
+  typedef typename Bits<sizeof(T) * V>::type B;
+  Pack<T, V> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.e[i] = from_f<T>(f[i]);
+  __builtin_nontemporal_store(__builtin_bit_cast(B, r), (B*)p);
+}
 template <typename T, int V>
 __device__ __forceinline__ void unpack(const Pack<T, V>& p, float* f) {
 #pragma unroll
@@ -72,19 +98,12 @@ __device__ __forceinline__ float sigmoid(float x) {
   return p;
 }
 
-// sigmoid(x) where it only scales a value that is then rounded to two bytes:
-// the exponent's and the reciprocal's own errors, some 2^-23 (1 + |x| / 2)
-// relative, lie far below that rounding, 2^-12 at best.
-__device__ __forceinline__ float sigmoid_rough(float x) {
-  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+// sigmoid(x) where it scales a value once: off by some (4 + 1.25 |x|) 2^-24 of
+// itself, by 5 * 2^-24 at most (the exponent's rounding, the exponential, the
+// reciprocal), at half the instructions.
+__device__ __forceinline__ float sigmoid_once(float x) {
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269502162933349609f);
   return __builtin_amdgcn_rcpf(1.f + e);
-}
-template <typename O>
-__device__ __forceinline__ float out_gate(float x) {
-  if constexpr (sizeof(O) == 2)
-    return sigmoid_rough(x);
-  else
-    return sigmoid(x);
 }
 
 // f(z) and its derivative for the activation ACT (ST_ACT_*).
@@ -93,7 +112,7 @@ __device__ __forceinline__ float act_fwd(float z) {
   if constexpr (ACT == ST_ACT_RELU)
     return z < 0.f ? 0.f : z;  // NaN stays
   else if constexpr (ACT == ST_ACT_SILU)
-    return z * sigmoid(z);
+    return z * sigmoid_once(z);
   else
     return z;
 }
@@ -102,14 +121,25 @@ __device__ __forceinline__ float act_grad(float z) {
   if constexpr (ACT == ST_ACT_RELU) {
     return z > 0.f ? 1.f : 0.f;
   } else if constexpr (ACT == ST_ACT_SILU) {
-    float p, n;
-    sigmoids(z, p, n);
-    // far out the product of a small and a large factor: z n -> 0
-    const float zn = n == 0.f ? 0.f : z * n;
-    return p * (1.f + zn);
+    // p (1 + z n), n = sigmoid(-z) = e p rather than 1 - p, whose error z
+    // would magnify; where e is large p is next to zero, and so is the result
+    const float e = __builtin_amdgcn_exp2f(z * -1.44269502162933349609f);
+    const float p = __builtin_amdgcn_rcpf(1.f + e);
+    return p * __builtin_fmaf(z, fminf(e, 0x1p100f) * p, 1.f);
   } else {
     return 1.f;
   }
+}
+
+// Calls f(std::integral_constant<int, ACT>{}) for the activation act.
+template <class F>
+__device__ __forceinline__ void with_activation_of(int act, F&& f) {
+  if (act == ST_ACT_RELU)
+    f(std::integral_constant<int, ST_ACT_RELU>{});
+  else if (act == ST_ACT_SILU)
+    f(std::integral_constant<int, ST_ACT_SILU>{});
+  else
+    f(std::integral_constant<int, ST_ACT_NONE>{});
 }
 
 // -------------------------------------------------------------- host side

@@ -4,9 +4,13 @@ their definitions read, each with a bound on what 32-bit arithmetic may add.
 Every function returns {name: (value, bound)}: `bound` is the absolute error
 that rounded 32-bit steps can reach, without the final rounding to the output
 type (half a step, added by `check`).  U = 2^-24 is half a step of a 32-bit
-value of magnitude one.  A sigmoid or its derivative is taken to be within
-SIG = 8 U of itself, relative (exponential 2 U, sum and quotient 2 U each, the
-rest spare)."""
+value of magnitude one.  A forget gate is taken to be within SIG = 8 U of
+itself, relative (exponential 2 U, sum and quotient 2 U each, the rest spare).
+A sigmoid that scales a value once (SiLU, the output gate) is within
+SIG + 1.25 U |x| of itself: its exponent x log2 e is rounded to half a step of
+itself, U |x| of the exponential, and so is log2 e, U |x| / 4.  The derivative
+of SiLU, p (1 + x n), is within SIG of a true one in absolute terms: where such
+a factor is off by more, x e^-|x| has made the term small."""
 
 import numpy as np
 import torch
@@ -50,6 +54,11 @@ def sig(x):
     with np.errstate(over="ignore"):
         e = np.exp(-np.abs(x))
     return np.where(x >= 0, 1 / (1 + e), e / (1 + e))
+
+
+def once(z, a=SILU):
+    """Relative bound of what a sigmoid of z scaled."""
+    return SIG + 1.25 * U * np.abs(z) if a == SILU else SIG
 
 
 def act(z, a):
@@ -98,7 +107,7 @@ def group_norm(x, groups, gamma, beta, a, eps):
             np.abs(v - m4) * e_rstd[:, None, :, None]).reshape(x.shape)
     e_z = np.abs(g) * e_xh + 4 * U * (np.abs(xh * g) + np.abs(b))
     y = act(z, a)
-    return {"y": (y, 1.1 * e_z + SIG * np.abs(y)), "mean": (mean, e_mean),
+    return {"y": (y, 1.1 * e_z + once(z, a) * np.abs(y)), "mean": (mean, e_mean),
             "rstd": (rstd, e_rstd)}
 
 
@@ -169,7 +178,7 @@ def time_conv(x, w, bias, a, window=None, lengths=None, reset=None,
                              np.abs(bias))
         out = act(z, a)
         y[time[live], rows[live]] = out[live]
-        e[time[live], rows[live]] = (1.1 * e_z + SIG * np.abs(out))[live]
+        e[time[live], rows[live]] = (1.1 * e_z + once(z, a) * np.abs(out))[live]
         win = np.where(live[None, :, None], taps[1:], win)
     return {"y": (y, e), "window": (win, 0.0)}
 
@@ -244,9 +253,11 @@ def gated_scan(v, f, o, h=None, lengths=None, reset=None, reverse=False):
         e = np.where(l2, keep * e + 2 * SIG * (keep * mag + add), e)
         mag = np.where(l2, keep * mag + add, mag)
         h = np.where(l2, new, h)
-        g = np.ones((b, c)) if o is None else sig(o[time, rows])
+        g, e_g = np.ones((b, c)), SIG
+        if o is not None:
+            g, e_g = sig(o[time, rows]), once(o[time, rows])
         y[time[live], rows[live]] = (h * g)[live]
-        e_y[time[live], rows[live]] = (g * (e + 2 * SIG * np.abs(h)))[live]
+        e_y[time[live], rows[live]] = (g * (e + 2 * e_g * np.abs(h)))[live]
     if not states:
         states, e_states = np.zeros((0, b, c)), np.zeros((0, b, c))
     return {"y": (y, e_y), "h": (h, e),

@@ -42,7 +42,7 @@ def norm(d=None, x=None, y=None, gamma=None, mean=None, rstd=None,
     (dict(dtype=1, out_dtype=0), "types"),
     (dict(dtype=1, out_dtype=2), "types"), (dict(n=-1), "sizes"),
     (dict(h=0), "sizes"), (dict(w=-2), "sizes"), (dict(c=0), "sizes"),
-    (dict(groups=0), "groups"), (dict(groups=3), "groups"),
+    (dict(n=1 << 20, c=1 << 11), "2^31"), (dict(groups=0), "groups"), (dict(groups=3), "groups"),
     (dict(act=3), "activation"), (dict(act=-1), "activation"),
     (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"),
     (dict(eps=float("inf")), "eps")])
