@@ -38,6 +38,7 @@ SOURCES = [
     ("../csrc_ops/time_conv.hip", EXACT),
     ("../csrc_ops/time_conv_grad.hip", EXACT),
     ("../csrc_ops/gated_scan.hip", EXACT),
+    ("../csrc_ops/gated_scan_grad.hip", EXACT),
 ]
 
 

@@ -1,0 +1,334 @@
+// The gated linear recurrence: what its forward and backward kernels share.
+#pragma once
+
+#include "seq.h"
+
+namespace st {
+namespace ops {
+
+constexpr int kStride = ST_SCAN_STRIDE;
+constexpr int kScanThreads = 256;
+
+struct ScanArgs {
+  SeqAxes q;
+  SeqTensor v, f, o, y;            // y: dy in the backward pass
+  SeqTensor dv, df, d_o;
+  const float* h;                  // backward: dh_out
+  float* h_out;                    // backward: dh
+  float* states;
+  int cv;
+  int64_t lanes;                   // b * cv
+  // rows split along time
+  int cols;                        // blocks of 64 lanes
+  int tiles, group;                // tiles of a row, tiles of a group
+  void* ends;                      // the ticket, then words: tiles, groups
+  int narrow;                      // 32-bit offsets within one time
+};
+constexpr int kHeadWords = 2;
+
+// ------------------------------------------------- rows split along time
+//
+// Few rows and channels, many steps: a thread for each would leave the device
+// idle.  h_s = a_s h_{s-1} + u_s joins: a run of steps acts as h -> A h + H
+// with A the product of its a (d -> A d + D for the gradient, whose order is
+// the reverse).  A block takes a tile: 64 lanes (V adjacent channels of a row
+// each) over W waves, a wave kSplit steps of every lane.  Gates and inputs of
+// these steps stay in registers, so that all is read once and every gate
+// computed once; the tile's (A, H) is published, those of the tiles before it
+// are folded, and the steps are run from the state that enters.
+//
+// Tiles are numbered by a ticket, so a block only waits for blocks that run
+// already, and these publish before they wait for anything themselves.  The
+// fold is in two levels, groups of `group` tiles and the tiles of the block's
+// own group, both in running order and cut by sizes alone: the same bits in
+// every run.  (Publishing states instead, each from the one before, would be
+// a chain of as many memory round trips as there are tiles; taking whatever
+// is there first would change the order of the roundings.)
+
+constexpr int kSplit = ST_SCAN_STRIDE;   // steps of a wave
+
+// A reset is a factor of minus zero (gates are never negative), which no value
+// passes, not even NaN.
+constexpr float kCut = -0.f;
+__device__ __forceinline__ bool is_cut(float A) {
+  return __float_as_uint(A) == 0x80000000u;
+}
+
+// (A, H), then (x, y): the steps of (x, y) run after those of (A, H).
+template <int V>
+__device__ __forceinline__ void then(float* A, float* H, const float* x,
+                                     const float* y) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const bool cut = is_cut(x[e]);
+    H[e] = cut ? y[e] : __builtin_fmaf(x[e], H[e], y[e]);
+    A[e] = cut ? x[e] : A[e] * x[e];
+  }
+}
+template <int V>
+__device__ __forceinline__ void none(float* A, float* H) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    A[e] = 1.f;
+    H[e] = 0.f;
+  }
+}
+
+// A published value: its bits beside a mark, in one 8-byte word, so that it
+// is whole when it is seen.  Words start as zeros.
+typedef unsigned long long Word;
+__device__ __forceinline__ void publish(Word* w, float x) {
+  __hip_atomic_store(w, (1ull << 32) | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Word peek(const Word* w) {
+  return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The places of published (A, H): entry i of this block's lanes.
+struct Ends {
+  Word* base;        // of entry 0, this lane
+  int64_t plane;     // words of an entry's A (its H follows)
+};
+template <int V>
+__device__ __forceinline__ void put_entry(const Ends& p, int64_t i,
+                                          const float* A, const float* H) {
+  Word* w = p.base + i * 2 * p.plane;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    publish(w + e, A[e]);
+    publish(w + p.plane + e, H[e]);
+  }
+}
+// Folds entries [i0, i1) into (A, H), two at a time, waiting for each.  (Few
+// registers: the gates of the block's steps are held meanwhile.)
+template <int V>
+__device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
+                                             float* A, float* H) {
+  const Word* q = p.base + (int64_t)i0 * 2 * p.plane;
+  for (int i = i0; i < i1; i += 2) {
+    const int64_t next = i + 1 < i1 ? 2 * p.plane : 0;
+    Word w[2][2 * V];
+    bool all;
+    do {
+      all = true;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          w[k][e] = peek(q + k * next + e);
+          w[k][V + e] = peek(q + k * next + p.plane + e);
+        }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) all = all && (w[k][e] >> 32) != 0;
+      if (!all) __builtin_amdgcn_s_sleep(1);
+    } while (!all);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (i + k < i1) {
+        float x[V], y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          x[e] = __uint_as_float((uint32_t)w[k][e]);
+          y[e] = __uint_as_float((uint32_t)w[k][V + e]);
+        }
+        then<V>(A, H, x, y);
+      }
+    }
+    q += 2 * next;
+  }
+}
+
+// A block's lanes and waves, in running order: wave 0 has the first steps to
+// run (of the backward pass: the row's last).
+template <int V, int W>
+struct TileShared {
+  float a[W][64 * V], h[W][64 * V];
+  int ticket;
+};
+
+// Joins the waves' (A, H) in LDS: each wave gets what runs before it in `A, H`
+// and every wave the whole in `TA, TH`.
+template <int V, int W>
+__device__ __forceinline__ void join_waves(TileShared<V, W>& sh, int wave,
+                                           float* A, float* H, float* TA,
+                                           float* TH) {
+  const int at = (threadIdx.x & 63) * V;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    sh.a[wave][at + e] = A[e];
+    sh.h[wave][at + e] = H[e];
+  }
+  __syncthreads();
+  none<V>(TA, TH);
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w == wave) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        A[e] = TA[e];
+        H[e] = TH[e];
+      }
+    }
+    then<V>(TA, TH, &sh.a[w][at], &sh.h[w][at]);
+  }
+}
+
+// What enters this tile (its k-th in running order): the state `h` after all
+// tiles before it, given the tile's own (TA, TH).  h comes in as the state
+// before the first tile, which only tile 0 has (the row's state may be
+// replaced in place once the last tile has run).
+template <int V, int W>
+__device__ __forceinline__ void enter_tile(const ScanArgs& a,
+                                           TileShared<V, W>& sh, int k,
+                                           int col, int wave, float* TA,
+                                           float* TH, float* h) {
+  if (a.tiles == 1) return;
+  Ends p;
+  p.plane = (int64_t)a.cols * 64 * V;
+  p.base = (Word*)a.ends + kHeadWords +
+           ((int64_t)col * 64 + (threadIdx.x & 63)) * V;
+  if (k == 0) {
+    // nothing enters but h: the tile's end is a state
+    if (wave == 0) {
+      float cut[V], end[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        cut[e] = kCut;
+        end[e] = is_cut(TA[e]) ? TH[e] : __builtin_fmaf(TA[e], h[e], TH[e]);
+      }
+      put_entry<V>(p, 0, cut, end);
+    }
+    return;
+  }
+  if (wave == 0) put_entry<V>(p, k, TA, TH);
+  const int g = k / a.group, in = k % a.group;
+  float A[V], H[V], PA[V], PH[V];
+  // the tiles of its group before it, a share to each wave
+  none<V>(A, H);
+  const int share = (in + W - 1) / W;
+  const int g0 = g * a.group;
+  fold_entries<V>(p, g0 + min(wave * share, in),
+                  g0 + min((wave + 1) * share, in), A, H);
+  join_waves<V, W>(sh, wave, A, H, PA, PH);
+  if (in == a.group - 1 && wave == 0 && k < a.tiles - 1) {
+    // the last of its group publishes the group
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      A[e] = PA[e];
+      H[e] = PH[e];
+    }
+    then<V>(A, H, TA, TH);
+    put_entry<V>(p, (int64_t)a.tiles + g, A, H);
+  }
+  // the groups before its own
+  none<V>(A, H);
+  const int gs = (g + W - 1) / W;
+  fold_entries<V>(p, a.tiles + min(wave * gs, g),
+                  a.tiles + min((wave + 1) * gs, g), A, H);
+  float GA[V], GH[V];
+  join_waves<V, W>(sh, wave, A, H, GA, GH);
+  then<V>(GA, GH, PA, PH);
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = GH[e];
+}
+
+struct LaneAt {
+  int b, ch;
+  bool on;          // otherwise a copy of the last lane that stores nothing
+  int64_t hc;
+};
+__device__ __forceinline__ LaneAt lane_at(const ScanArgs& a, int col,
+                                          int v) {
+  int64_t lane = (int64_t)col * 64 + (threadIdx.x & 63);
+  LaneAt l;
+  l.on = lane < a.lanes;
+  if (!l.on) lane = a.lanes - 1;
+  l.b = (int)(lane / a.cv);
+  l.ch = (int)(lane % a.cv) * v;
+  l.hc = (int64_t)l.b * a.q.c + l.ch;
+  return l;
+}
+template <int V, int W>
+__device__ __forceinline__ int next_ticket(const ScanArgs& a,
+                                           TileShared<V, W>& sh) {
+  if (a.tiles == 1) return blockIdx.x;
+  if (threadIdx.x == 0)
+    sh.ticket = (int)__hip_atomic_fetch_add((unsigned*)a.ends, 1u,
+                                            __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(sh.ticket);
+}
+// Whether all lanes of a wave have all of `steps` steps from s0 on, at the same
+// times, and the time of the first.
+struct Whole {
+  bool on;
+  int64_t t;
+  int dir;
+};
+__device__ __forceinline__ Whole whole_wave(const ScanArgs& a, const Row& r,
+                                            int s0, int steps) {
+  Whole w;
+  w.on = a.narrow && !(a.q.lengths && a.q.reverse) &&
+         __all(s0 + steps <= r.len);
+  w.t = a.q.reverse ? a.q.t - 1 - s0 : s0;
+  w.dir = a.q.reverse ? -1 : 1;
+  return w;
+}
+template <typename T, int V, int N>
+__device__ __forceinline__ void load_steps(const SeqTensor& x, const Whole& w,
+                                           const ScanArgs& a, const Row& r,
+                                           int b, int ch, int s0,
+                                           Pack<T, V>* out) {
+  if (w.on) {
+    const WaveWalk<const T> p(x, w.t, w.dir, b, ch);
+#pragma unroll
+    for (int k = 0; k < N; ++k) out[k] = load_pack<T, V>(p.at(k));
+  } else {
+    Walk<const T> p(x, r, b, ch, s0);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (s0 + k < a.q.t) {      // no row is longer
+        out[k] = load_pack<T, V>(p.p);
+        p.next();
+      }
+      // one address at a time, not all of them in registers first
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+// Bit k: a reset before step s0 + k.
+__device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
+                                            int b, int s0) {
+  unsigned m = 0;
+  if (a.q.reset) {
+    // all loads at once: none waits for another
+    const SeqTensor t{(void*)a.q.reset, a.q.b, 1};
+    Walk<const uint8_t> w(t, r, b, 0, s0);
+    uint8_t x[kSplit];
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k) {
+      x[k] = *w.p;
+      w.next();
+    }
+#pragma unroll
+    for (int k = 0; k < kSplit; ++k)
+      if (s0 + k < r.len && x[k]) m |= 1u << k;
+  }
+  return m;
+}
+
+// Launches (defined beside their kernels).  Rows split along time: blocks of
+// kWaves (backward: kGradWaves) waves.
+constexpr int kWaves = 8, kGradWaves = 4;
+void launch_scan(const ScanArgs& a, int dtype, int out_dtype, int vec,
+                 bool split, hipStream_t q);
+void launch_scan_backward(const ScanArgs& a, int dtype, int out_dtype,
+                          bool split, hipStream_t q);
+
+}  // namespace ops
+}  // namespace st

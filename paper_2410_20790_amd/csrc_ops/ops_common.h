@@ -106,6 +106,15 @@ __device__ __forceinline__ float sigmoid_once(float x) {
   return __builtin_amdgcn_rcpf(1.f + e);
 }
 
+// sigmoid(x) and sigmoid(-x) likewise.  (n as e p rather than 1 - p, whose
+// error a large factor would magnify; where e is that large p is next to zero,
+// and so is every result.)
+__device__ __forceinline__ void sigmoids_once(float x, float& p, float& n) {
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269502162933349609f);
+  p = __builtin_amdgcn_rcpf(1.f + e);
+  n = fminf(e, 0x1p100f) * p;
+}
+
 // f(z) and its derivative for the activation ACT (ST_ACT_*).
 template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {
@@ -121,11 +130,9 @@ __device__ __forceinline__ float act_grad(float z) {
   if constexpr (ACT == ST_ACT_RELU) {
     return z > 0.f ? 1.f : 0.f;
   } else if constexpr (ACT == ST_ACT_SILU) {
-    // p (1 + z n), n = sigmoid(-z) = e p rather than 1 - p, whose error z
-    // would magnify; where e is large p is next to zero, and so is the result
-    const float e = __builtin_amdgcn_exp2f(z * -1.44269502162933349609f);
-    const float p = __builtin_amdgcn_rcpf(1.f + e);
-    return p * __builtin_fmaf(z, fminf(e, 0x1p100f) * p, 1.f);
+    float p, n;
+    sigmoids_once(z, p, n);
+    return p * __builtin_fmaf(z, n, 1.f);
   } else {
     return 1.f;
   }

@@ -65,6 +65,12 @@ struct Walk {
   __device__ __forceinline__ void advance(int k) {  // from step s0 + k
     if (k < left) p += step;
   }
+  __device__ __forceinline__ void next() {          // likewise, one by one
+    if (left > 0) {
+      p += step;
+      --left;
+    }
+  }
 };
 
 // The same for a whole wave whose lanes all have the steps at one time: a

@@ -40,13 +40,15 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
     const int end = min(s1, r.len);
     float win[K > 1 ? K - 1 : 1][V];
     if (s0 < end) load_window<T, V, K>(a, r, b, ch, s0, win);
-    const T* x = (const T*)a.x.p + (int64_t)b * a.x.sb + ch;
-    O* y = (O*)a.y.p + (int64_t)b * a.y.sb + ch;
+    Walk<const T> wx(a.x, r, b, ch, s0);
+    Walk<O> wy(a.y, r, b, ch, s0);
     for (int s = s0; s < end; s += kAhead) {
       Pack<T, V> in[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        in[k] = load_pack<T, V>(x + time_of(r, min(s + k, end - 1)) * a.x.st);
+      for (int k = 0; k < kAhead; ++k) {
+        in[k] = load_pack<T, V>(wx.p);
+        wx.next();
+      }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         if (s + k < end) {
@@ -67,7 +69,8 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
             z[e] = __builtin_fmaf(w[K - 1][e], f[e], z[e]);
             z[e] = act_any(a.act, z[e]);
           }
-          store_pack<O, V>(y + time_of(r, s + k) * a.y.st, z);
+          store_pack<O, V>(wy.p, z);
+          wy.next();
 #pragma unroll
           for (int e = 0; e < V; ++e) {
 #pragma unroll
@@ -77,6 +80,7 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
         }
       }
     }
+    O* y = (O*)a.y.p + (int64_t)b * a.y.sb + ch;
     for (int s = max(s0, r.len); s < s1; ++s) {
       float z[V];
 #pragma unroll
@@ -94,7 +98,8 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
         const T* from = nullptr;
         if (p >= cut) {
           if (p >= 0)
-            from = x + time_of(r, p) * a.x.st;
+            from = (const T*)a.x.p + time_of(r, p) * a.x.st +
+                   (int64_t)b * a.x.sb + ch;
           else if (a.window)
             from = (const T*)a.window +
                    ((int64_t)(K - 1 + p) * a.q.b + b) * a.q.c + ch;
@@ -110,7 +115,11 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
 
 // -------------------------------------------------------------- host side
 
-constexpr int64_t kFillThreads = 256 * 1024;  // four waves per SIMD
+// Threads that fill the device: four waves to a SIMD; half as many in the
+// backward pass of wide vectors, whose tiles cost it more (a halo on both
+// sides, sums to join): 601 steps of 48 rows of 512 channels 43 us (52 with
+// as many; one channel to a thread loses, 45 for 38).
+constexpr int64_t kFillThreads = 256 * 1024;
 constexpr int kTargetBlocks = 1024;
 
 struct ConvCut {
@@ -127,8 +136,9 @@ ConvCut cut_of(const st_seq_desc& d, int taps, bool backward, int v) {
   // a tile's halo is taps - 1 steps: at least four times as many steps
   const int64_t lanes = (int64_t)d.b * c.cv;
   const int64_t least = std::max(8, 4 * (taps - 1));
-  const int64_t want = ceil_div((int64_t)d.t * std::max<int64_t>(lanes, 1),
-                                kFillThreads);
+  const int64_t fill = backward && v == 4 ? kFillThreads / 2 : kFillThreads;
+  const int64_t want =
+      ceil_div((int64_t)d.t * std::max<int64_t>(lanes, 1), fill);
   c.tile = (int)std::max(least, std::min<int64_t>(want, 1 << 20));
   c.tiles = (int)std::max<int64_t>(1, ceil_div(d.t, c.tile));
   const int64_t need = ceil_div((int64_t)c.tiles * d.b, c.rows);

@@ -44,9 +44,6 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
     const int tile = (int)(u / a.q.b);
     const Row r = row_of(a.q, b);
     const int s0 = tile * a.tile, s1 = min(s0 + a.tile, a.q.t);
-    const T* x = (const T*)a.x.p + (int64_t)b * a.x.sb + ch;
-    const O* dy = (const O*)a.dy.p + (int64_t)b * a.dy.sb + ch;
-    T* dx = a.dx.p ? (T*)a.dx.p + (int64_t)b * a.dx.sb + ch : nullptr;
     const int own = min(s1, r.len);             // steps [s0, own) are its own
     const int end = min(s1 + K - 1, r.len);     // steps it needs dz of
     const int first = tile == 0 ? -(K - 1) : s0;  // positions [first, own)
@@ -57,7 +54,8 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
     for (int i = 0; i < K; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[i][e] = 0.f;
-    // the finished dx of position p
+    // the finished dx of position p (in rising order)
+    Walk<T> dx(a.dx, r, b, ch, s0);
     auto put = [&](int p, float* v) {
       if (p < first || p >= own) return;
       const int i = p - (r.len - (K - 1));      // its place in window_out
@@ -70,7 +68,8 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
         for (int e = 0; e < V; ++e) v[e] += g[e];
       }
       if (p >= 0) {
-        if (dx) store_pack<T, V>(dx + time_of(r, p) * a.dx.st, v);
+        if (a.dx.p) store_pack<T, V>(dx.p, v);
+        dx.next();
       } else if (a.dwindow) {
         store_pack<T, V>((T*)a.dwindow +
                              ((int64_t)(K - 1 + p) * a.q.b + b) * a.q.c + ch,
@@ -81,14 +80,17 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
       int open = K;    // taps back that no reset hides
       if (s0 < own) load_window<T, V, K>(a, r, b, ch, s0, win);
       int s = s0;
+      Walk<const T> x(a.x, r, b, ch, s0);
+      Walk<const O> dy(a.dy, r, b, ch, s0);
       for (; s < end; s += kAhead) {
         Pack<T, V> xi[kAhead];
         Pack<O, V> di[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          const int64_t t = time_of(r, min(s + k, end - 1));
-          xi[k] = load_pack<T, V>(x + t * a.x.st);
-          di[k] = load_pack<O, V>(dy + t * a.dy.st);
+          xi[k] = load_pack<T, V>(x.p);
+          di[k] = load_pack<O, V>(dy.p);
+          x.next();
+          dy.next();
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -143,12 +145,13 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
 #pragma unroll
       for (int j = 0; j < K - 1; ++j) put(at - (K - 1) + j, acc[j]);
     }
-    if (dx) {
+    if (a.dx.p) {
+      T* q = (T*)a.dx.p + (int64_t)b * a.dx.sb + ch;
       for (int s = max(s0, r.len); s < s1; ++s) {
         float z[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) z[e] = 0.f;
-        store_pack<T, V>(dx + (int64_t)s * a.dx.st, z);
+        store_pack<T, V>(q + (int64_t)s * a.dx.st, z);
       }
     }
   }
@@ -174,22 +177,24 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
   }
 }
 
-// Sums the blocks' parts: 32 channels by 8 lanes of parts in a block.
+// Sums the blocks' parts in f64: 16 channels by 16 lanes of parts in a block.
 __global__ __launch_bounds__(256) void k_time_conv_join(ConvTimeArgs a,
                                                         int taps) {
-  __shared__ double red[8][32];
-  const int cx = threadIdx.x & 31, k = threadIdx.x >> 5;
+  __shared__ double red[16][16];
+  const int cx = threadIdx.x & 15, k = threadIdx.x >> 4;
   const int64_t total = (int64_t)(taps + 1) * a.q.c;
-  for (int64_t i0 = blockIdx.x * 32ll; i0 < total; i0 += gridDim.x * 32ll) {
+  for (int64_t i0 = blockIdx.x * 16ll; i0 < total; i0 += gridDim.x * 16ll) {
     const int64_t i = i0 + cx;
     double s = 0;
-    if (i < total)
-      for (int p = k; p < a.gridy; p += 8) s += a.part[p * total + i];
+    if (i < total) {
+#pragma unroll 8
+      for (int p = k; p < a.gridy; p += 16) s += a.part[p * total + i];
+    }
     __syncthreads();
     red[k][cx] = s;
     __syncthreads();
     if (k == 0 && i < total) {
-      for (int p = 1; p < 8; ++p) s += red[p][cx];
+      for (int p = 1; p < 16; ++p) s += red[p][cx];
       const int64_t j = i / a.q.c;
       if (j < taps) {
         if (a.dweight) a.dweight[i] = (float)s;
@@ -219,7 +224,7 @@ void launch_time_conv_backward(const ConvTimeArgs& a, int dtype,
     });
   if (a.dweight || a.dbias) {
     const int64_t total = (int64_t)(taps + 1) * a.q.c;
-    k_time_conv_join<<<(unsigned)std::min<int64_t>(ceil_div(total, 32), 4096),
+    k_time_conv_join<<<(unsigned)std::min<int64_t>(ceil_div(total, 16), 4096),
                        256, 0, stream>>>(a, taps);
   }
 }
