@@ -74,11 +74,15 @@ __device__ __forceinline__ void none(float* A, float* H) {
   }
 }
 
-// A published value: its bits beside a mark, in one 8-byte word, so that it
-// is whole when it is seen.  Words start as zeros.
+// A published (A, H) of a channel, in one 8-byte word, so that it is whole when
+// it is seen: H's bits below A's with the sign set, which no factor has (a
+// reset, minus zero, goes as minus infinity).  Words start as zeros.
 typedef unsigned long long Word;
-__device__ __forceinline__ void publish(Word* w, float x) {
-  __hip_atomic_store(w, (1ull << 32) | __float_as_uint(x), __ATOMIC_RELAXED,
+constexpr uint32_t kCutBits = 0xff800000u;
+__device__ __forceinline__ void publish(Word* w, float A, float H) {
+  const uint32_t hi =
+      is_cut(A) ? kCutBits : __float_as_uint(A) | 0x80000000u;
+  __hip_atomic_store(w, (Word)hi << 32 | __float_as_uint(H), __ATOMIC_RELAXED,
                      __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ Word peek(const Word* w) {
@@ -88,56 +92,51 @@ __device__ __forceinline__ Word peek(const Word* w) {
 // The places of published (A, H): entry i of this block's lanes.
 struct Ends {
   Word* base;        // of entry 0, this lane
-  int64_t plane;     // words of an entry's A (its H follows)
+  int64_t plane;     // words of an entry
 };
 template <int V>
 __device__ __forceinline__ void put_entry(const Ends& p, int64_t i,
                                           const float* A, const float* H) {
-  Word* w = p.base + i * 2 * p.plane;
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    publish(w + e, A[e]);
-    publish(w + p.plane + e, H[e]);
-  }
+  for (int e = 0; e < V; ++e) publish(p.base + i * p.plane + e, A[e], H[e]);
 }
-// Folds entries [i0, i1) into (A, H), two at a time, waiting for each.  (Few
-// registers: the gates of the block's steps are held meanwhile.)
+// Folds entries [i0, i1) into (A, H), four at a time, waiting for each.
 template <int V>
 __device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
                                              float* A, float* H) {
-  const Word* q = p.base + (int64_t)i0 * 2 * p.plane;
-  for (int i = i0; i < i1; i += 2) {
-    const int64_t next = i + 1 < i1 ? 2 * p.plane : 0;
-    Word w[2][2 * V];
+  constexpr int N = 4 / V;
+  const Word* q = p.base + (int64_t)i0 * p.plane;
+  for (int i = i0; i < i1; i += N) {
+    Word w[N][V];
     bool all;
     do {
       all = true;
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < N; ++k) {
+        const Word* x = q + (int64_t)min(k, i1 - 1 - i) * p.plane;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          w[k][e] = peek(q + k * next + e);
-          w[k][V + e] = peek(q + k * next + p.plane + e);
-        }
+        for (int e = 0; e < V; ++e) w[k][e] = peek(x + e);
+      }
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < N; ++k)
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) all = all && (w[k][e] >> 32) != 0;
+        for (int e = 0; e < V; ++e) all = all && (w[k][e] >> 63) != 0;
       if (!all) __builtin_amdgcn_s_sleep(1);
     } while (!all);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < N; ++k) {
       if (i + k < i1) {
         float x[V], y[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          x[e] = __uint_as_float((uint32_t)w[k][e]);
-          y[e] = __uint_as_float((uint32_t)w[k][V + e]);
+          const uint32_t hi = (uint32_t)(w[k][e] >> 32);
+          x[e] = hi == kCutBits ? kCut : __uint_as_float(hi & 0x7fffffffu);
+          y[e] = __uint_as_float((uint32_t)w[k][e]);
         }
         then<V>(A, H, x, y);
       }
     }
-    q += 2 * next;
+    q += N * p.plane;
   }
 }
 
@@ -302,6 +301,7 @@ __device__ __forceinline__ void load_steps(const SeqTensor& x, const Whole& w,
   }
 }
 // Bit k: a reset before step s0 + k.
+template <int N>
 __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
                                             int b, int s0) {
   unsigned m = 0;
@@ -309,14 +309,14 @@ __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
     // all loads at once: none waits for another
     const SeqTensor t{(void*)a.q.reset, a.q.b, 1};
     Walk<const uint8_t> w(t, r, b, 0, s0);
-    uint8_t x[kSplit];
+    uint8_t x[N];
 #pragma unroll
-    for (int k = 0; k < kSplit; ++k) {
+    for (int k = 0; k < N; ++k) {
       x[k] = *w.p;
       w.next();
     }
 #pragma unroll
-    for (int k = 0; k < kSplit; ++k)
+    for (int k = 0; k < N; ++k)
       if (s0 + k < r.len && x[k]) m |= 1u << k;
   }
   return m;

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   float A[V], H[V], TA[V], TH[V];
   none<V>(A, H);
   if (any) {
-    cuts = cuts_of(a, r, l.b, s0);
+    cuts = cuts_of<kSplit>(a, r, l.b, s0);
     Pack<T, V> iv[kSplit], jf[kSplit];
     load_steps<T, V, kSplit>(a.f, whole, a, r, l.b, l.ch, s0, jf);
     load_steps<T, V, kSplit>(a.v, whole, a, r, l.b, l.ch, s0, iv);
@@ -249,30 +249,33 @@ void with_scan(int v, bool gate, F&& f) {
 constexpr int kSerialSteps = 64;
 constexpr int64_t kFillWaves = 2048;    // eight to a CU
 
+constexpr int kTile = kSplit * kWaves, kGradTile = kSplit * kGradWaves;
+
 struct ScanCut {
   bool split = false;
   int cols = 0, tiles = 0, group = 0;
   uint64_t words = 0;
 };
-ScanCut cut_of(const st_seq_desc& d, int waves) {
+ScanCut cut_of(const st_seq_desc& d, int steps) {
   ScanCut c;
   const int64_t cols = ceil_div((int64_t)d.b * d.c, 64);
   if (d.t <= kSerialSteps || cols >= kFillWaves) return c;
   c.split = true;
   c.cols = (int)cols;
-  c.tiles = (int)ceil_div(d.t, (int64_t)kSplit * waves);
+  c.tiles = (int)ceil_div(d.t, steps);
   // a block folds at most group tiles and tiles / group groups
   c.group = 8;
   while ((int64_t)c.group * c.group < c.tiles) c.group *= 2;
   if (c.tiles > 1)
-    c.words = kHeadWords + (uint64_t)(c.tiles + c.tiles / c.group) * 2 *
-                               c.cols * 64;
+    c.words = kHeadWords +
+              (uint64_t)(c.tiles + c.tiles / c.group) * c.cols * 64;
   return c;
 }
 
 uint64_t scan_space(const st_seq_desc& d, bool backward) {
   if (empty(d)) return 0;
-  return (cut_of(d, backward ? kGradWaves : kWaves).words * 8 + 15) / 16 * 16;
+  const uint64_t words = cut_of(d, backward ? kGradTile : kTile).words;
+  return (words * 8 + 15) / 16 * 16;
 }
 
 // Channels to a lane of rows that are walked: as many as a vector has, while
@@ -381,7 +384,7 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.h_out = h_out;
     a.states = states;
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, kWaves);
+    const ScanCut cut = cut_of(*d, kTile);
     vec = cut.split ? 1 : lane_vec(*d, vec);
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
@@ -459,7 +462,7 @@ extern "C" st_status st_gated_scan_backward(
     a.h_out = dh;
     a.states = const_cast<float*>(states);
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, kGradWaves);
+    const ScanCut cut = cut_of(*d, kGradTile);
     a.cv = d->c;
     a.lanes = (int64_t)d->b * d->c;
     take_cut(a, cut, ws, q);

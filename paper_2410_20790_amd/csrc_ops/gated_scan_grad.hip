@@ -45,7 +45,7 @@ struct GradSteps {
           load_pack<float, V>(a.states + (s0 / kStride) *
                                   ((int64_t)a.q.b * a.q.c) + l.hc),
           h);
-    cuts = cuts_of(a, r, l.b, s0);
+    cuts = cuts_of<kSplit>(a, r, l.b, s0);
     auto step = [&](int k, float* go) {
       const bool cut = cuts >> k & 1;
       float v[V], f[V], o[V];

@@ -115,11 +115,11 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
 
 // -------------------------------------------------------------- host side
 
-// Threads that fill the device: four waves to a SIMD; half as many in the
-// backward pass of wide vectors, whose tiles cost it more (a halo on both
-// sides, sums to join): 601 steps of 48 rows of 512 channels 43 us (52 with
-// as many; one channel to a thread loses, 45 for 38).
-constexpr int64_t kFillThreads = 256 * 1024;
+constexpr int64_t kFillThreads = 256 * 1024;  // four waves to a SIMD
+// Channels to a thread of the backward pass, whose registers hold three
+// windows: two measured 46 us where four take 53 and one 57 (gradients of
+// 20000 steps of 1024 channels bf16).
+constexpr int kGradVec = 2;
 constexpr int kTargetBlocks = 1024;
 
 struct ConvCut {
@@ -136,9 +136,8 @@ ConvCut cut_of(const st_seq_desc& d, int taps, bool backward, int v) {
   // a tile's halo is taps - 1 steps: at least four times as many steps
   const int64_t lanes = (int64_t)d.b * c.cv;
   const int64_t least = std::max(8, 4 * (taps - 1));
-  const int64_t fill = backward && v == 4 ? kFillThreads / 2 : kFillThreads;
-  const int64_t want =
-      ceil_div((int64_t)d.t * std::max<int64_t>(lanes, 1), fill);
+  const int64_t want = ceil_div((int64_t)d.t * std::max<int64_t>(lanes, 1),
+                                kFillThreads);
   c.tile = (int)std::max(least, std::min<int64_t>(want, 1 << 20));
   c.tiles = (int)std::max<int64_t>(1, ceil_div(d.t, c.tile));
   const int64_t need = ceil_div((int64_t)c.tiles * d.b, c.rows);
@@ -162,7 +161,7 @@ st_status check_conv(const st_seq_desc* d, int32_t taps, int32_t act) {
 uint64_t conv_space(const st_seq_desc& d, int taps, bool backward) {
   if (!backward || d.b == 0) return 0;
   uint64_t most = 0;
-  for (int v = 4; v >= 1; v /= 2)
+  for (int v = kGradVec; v >= 1; v /= 2)
     if (d.c % v == 0)
       most = std::max<uint64_t>(most, cut_of(d, taps, true, v).part_bytes);
   return most;
@@ -283,7 +282,7 @@ extern "C" st_status st_time_conv_backward(
       return bad("an output overlaps an input, another output or the "
                  "workspace");
     (void)hipGetLastError();
-    int v = 4;
+    int v = kGradVec;
     for (; v > 1; v /= 2)
       if (d->c % v == 0 && ops::vec_ok(v, es, *d, x) &&
           ops::vec_ok(v, eo, *d, dy) && ops::vec_ok(v, es, *d, dx) &&

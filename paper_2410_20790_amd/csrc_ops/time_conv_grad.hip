@@ -82,16 +82,28 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
       int s = s0;
       Walk<const T> x(a.x, r, b, ch, s0);
       Walk<const O> dy(a.dy, r, b, ch, s0);
+      // the next steps' loads are in flight while these are worked on
+      Pack<T, V> xn[kAhead];
+      Pack<O, V> dn[kAhead];
+      auto fetch = [&] {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          xn[k] = load_pack<T, V>(x.p);
+          dn[k] = load_pack<O, V>(dy.p);
+          x.next();
+          dy.next();
+        }
+      };
+      if (s < end) fetch();
       for (; s < end; s += kAhead) {
         Pack<T, V> xi[kAhead];
         Pack<O, V> di[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          xi[k] = load_pack<T, V>(x.p);
-          di[k] = load_pack<O, V>(dy.p);
-          x.next();
-          dy.next();
+          xi[k] = xn[k];
+          di[k] = dn[k];
         }
+        if (s + kAhead < end) fetch();
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           if (s + k < end) {
@@ -217,8 +229,9 @@ void launch_time_conv_backward(const ConvTimeArgs& a, int dtype,
       using O = typename decltype(to)::type;
       with_conv_vec(vec, [&](auto vt) {
         with_taps(taps, [&](auto kt) {
-          k_time_conv_grad<T, O, decltype(vt)::value, decltype(kt)::value>
-              <<<grid, kConvThreads, 0, stream>>>(a);
+          if constexpr (decltype(vt)::value <= 2)
+            k_time_conv_grad<T, O, decltype(vt)::value, decltype(kt)::value>
+                <<<grid, kConvThreads, 0, stream>>>(a);
         });
       });
     });
