@@ -483,8 +483,8 @@ typedef struct st_seq_ref {
   int64_t stride_t, stride_b;
 } st_seq_ref;
 
-/* The axes of a sequence operator.  t and b may be 0; c at least 1; b * c
- * below 2^31.
+/* The axes of a sequence operator.  t (at most 2^30) and b may be 0; c at
+ * least 1; b * c below 2^31.
  *   lengths  device int32 [b], or NULL (every row has t steps): row i has
  *            lengths[i] steps (values outside [0, t] count as the nearer
  *            bound).  What lies behind them is not read; outputs behind

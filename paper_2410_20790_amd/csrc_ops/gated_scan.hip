@@ -248,6 +248,7 @@ void with_scan(int v, bool gate, F&& f) {
 // each.
 constexpr int kSerialSteps = 64;
 constexpr int64_t kFillWaves = 2048;    // eight to a CU
+constexpr int64_t kMaxBlocks = 1 << 22;
 
 constexpr int kTile = kSplit * kWaves, kGradTile = kSplit * kGradWaves;
 
@@ -260,6 +261,8 @@ ScanCut cut_of(const st_seq_desc& d, int steps) {
   ScanCut c;
   const int64_t cols = ceil_div((int64_t)d.b * d.c, 64);
   if (d.t <= kSerialSteps || cols >= kFillWaves) return c;
+  // (as many blocks as a launch may have; beyond that, rows are walked)
+  if (cols * ceil_div(d.t, steps) > kMaxBlocks) return c;
   c.split = true;
   c.cols = (int)cols;
   c.tiles = (int)ceil_div(d.t, steps);
@@ -342,16 +345,22 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
                                    uint64_t ws_bytes, void* stream) {
   return guarded([&]() -> st_status {
     if (const st_status s = check_seq(d); s != ST_OK) return s;
-    if (const st_status s = check_ref(*d, v, false, "v"); s != ST_OK) return s;
-    if (const st_status s = check_ref(*d, f, false, "f"); s != ST_OK) return s;
+    const int es = esize(d->dtype), eo = esize(d->out_dtype);
+    if (const st_status s = check_ref(*d, v, es, false, "v"); s != ST_OK)
+      return s;
+    if (const st_status s = check_ref(*d, f, es, false, "f"); s != ST_OK)
+      return s;
     if (o)
-      if (const st_status s = check_ref(*d, o, false, "o"); s != ST_OK)
+      if (const st_status s = check_ref(*d, o, es, false, "o"); s != ST_OK)
         return s;
-    if (const st_status s = check_ref(*d, y, true, "y"); s != ST_OK) return s;
+    if (const st_status s = check_ref(*d, y, eo, true, "y"); s != ST_OK)
+      return s;
+    if (const st_status s = check_addresses({h, h_out, states}, {}, es);
+        s != ST_OK)
+      return s;
     if (const st_status s = check_ws(scan_space(*d, false), ws, ws_bytes);
         s != ST_OK)
       return s;
-    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     const int64_t plane = (int64_t)d->b * d->c * 4;
     const Span sh = span_of(h, plane);
     if (any_hit({ref_span(*d, y, eo), span_of(h_out, plane),
@@ -402,24 +411,25 @@ extern "C" st_status st_gated_scan_backward(
     void* stream) {
   return guarded([&]() -> st_status {
     if (const st_status s = check_seq(d); s != ST_OK) return s;
-    struct { const st_seq_ref* r; bool out; const char* name; } refs[] = {
-        {dy, false, "dy"}, {v, false, "v"},   {f, false, "f"},
-        {dv, true, "dv"},  {df, true, "df"}};
-    for (const auto& x : refs)
-      if (const st_status s = check_ref(*d, x.r, x.out, x.name); s != ST_OK)
-        return s;
+    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     if (!o != !d_o) return bad("o and d_o: both or neither");
-    if (o) {
-      if (const st_status s = check_ref(*d, o, false, "o"); s != ST_OK)
+    struct { const st_seq_ref* r; int es; bool out; const char* name; }
+    refs[] = {{dy, eo, false, "dy"}, {v, es, false, "v"},
+              {f, es, false, "f"},   {dv, es, true, "dv"},
+              {df, es, true, "df"},  {o, es, false, "o"},
+              {d_o, es, true, "d_o"}};
+    for (int i = 0; i < (o ? 7 : 5); ++i)
+      if (const st_status s = check_ref(*d, refs[i].r, refs[i].es,
+                                        refs[i].out, refs[i].name);
+          s != ST_OK)
         return s;
-      if (const st_status s = check_ref(*d, d_o, true, "d_o"); s != ST_OK)
-        return s;
-    }
+    if (const st_status s = check_addresses({states, dh_out, dh}, {}, es);
+        s != ST_OK)
+      return s;
     if (!states && !empty(*d)) return bad("states is NULL");
     if (const st_status s = check_ws(scan_space(*d, true), ws, ws_bytes);
         s != ST_OK)
       return s;
-    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     const int64_t plane = (int64_t)d->b * d->c * 4;
     const std::initializer_list<Span> in = {
         ref_span(*d, dy, eo), ref_span(*d, v, es), ref_span(*d, f, es),

@@ -497,9 +497,10 @@ int64_t reach(const st_norm_desc& d, const st_map_ref& m) {
   return (d.n - 1) * m.stride_n + (d.h - 1) * m.stride_h +
          (d.w - 1) * m.stride_w + d.c;
 }
-st_status check_map(const st_norm_desc& d, const st_map_ref* m, bool out,
-                    const char* name) {
+st_status check_map(const st_norm_desc& d, const st_map_ref* m, int es,
+                    bool out, const char* name) {
   if (!m || !m->data) return bad(std::string(name) + " is NULL");
+  if (!aligned(m->data, es)) return bad(std::string(name) + " is misaligned");
   if (m->stride_n < 0 || m->stride_h < 0 || m->stride_w < 0)
     return bad(std::string(name) + " has a negative stride");
   if (!out) return ST_OK;
@@ -649,12 +650,17 @@ extern "C" st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
   return guarded([&]() -> st_status {
     if (const st_status s = check_desc(d); s != ST_OK) return s;
     if (d->n == 0) return ST_OK;
-    if (const st_status s = check_map(*d, x, false, "x"); s != ST_OK) return s;
-    if (const st_status s = check_map(*d, y, true, "y"); s != ST_OK) return s;
+    const int es = esize(d->dtype), eo = esize(d->out_dtype);
+    if (const st_status s = check_map(*d, x, es, false, "x"); s != ST_OK)
+      return s;
+    if (const st_status s = check_map(*d, y, eo, true, "y"); s != ST_OK)
+      return s;
+    for (const void* p : {(const void*)gamma, (const void*)beta,
+                          (const void*)mean, (const void*)rstd})
+      if (!aligned(p, 4)) return bad("an array of floats is misaligned");
     if (!mean != !rstd) return bad("mean and rstd: both or neither");
     if (const st_status s = check_space(*d, false, ws, ws_bytes); s != ST_OK)
       return s;
-    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     const int64_t ng = (int64_t)d->n * d->groups * 4;
     const Span sy = map_span(*d, *y, eo), sm = span_of(mean, ng),
                sr = span_of(rstd, ng), sw = span_of(ws, (int64_t)ws_bytes),
@@ -698,6 +704,11 @@ extern "C" st_status st_group_norm_backward(
     void* ws, uint64_t ws_bytes, void* stream) {
   return guarded([&]() -> st_status {
     if (const st_status s = check_desc(d); s != ST_OK) return s;
+    const int es = esize(d->dtype), eo = esize(d->out_dtype);
+    for (const void* p : {(const void*)gamma, (const void*)beta,
+                          (const void*)mean, (const void*)rstd,
+                          (const void*)dgamma, (const void*)dbeta})
+      if (!aligned(p, 4)) return bad("an array of floats is misaligned");
     hipStream_t q = (hipStream_t)stream;
     NormArgs a{};
     a.dgamma = dgamma;
@@ -715,15 +726,15 @@ extern "C" st_status st_group_norm_backward(
       }
       return ST_OK;
     }
-    if (const st_status s = check_map(*d, dy, false, "dy"); s != ST_OK)
+    if (const st_status s = check_map(*d, dy, eo, false, "dy"); s != ST_OK)
       return s;
-    if (const st_status s = check_map(*d, x, false, "x"); s != ST_OK) return s;
-    if (const st_status s = check_map(*d, dx, true, "dx"); s != ST_OK)
+    if (const st_status s = check_map(*d, x, es, false, "x"); s != ST_OK)
+      return s;
+    if (const st_status s = check_map(*d, dx, es, true, "dx"); s != ST_OK)
       return s;
     if (!mean || !rstd) return bad("mean or rstd is NULL");
     if (const st_status s = check_space(*d, true, ws, ws_bytes); s != ST_OK)
       return s;
-    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     const int64_t ng = (int64_t)d->n * d->groups * 4, cb = d->c * 4ll;
     const Span in[] = {map_span(*d, *dy, eo), map_span(*d, *x, es),
                        span_of(mean, ng),     span_of(rstd, ng),

@@ -193,6 +193,9 @@ inline Span span_of(const void* p, int64_t bytes) {
   return p ? Span{(const char*)p, (const char*)p + bytes} : Span{};
 }
 
+// Whether an address that may be absent is one of elements of `es` bytes.
+inline bool aligned(const void* p, int es) { return (uintptr_t)p % es == 0; }
+
 // Calls f(type tags) for a known pair of data types.
 template <typename T> struct Tag { using type = T; };
 template <class F>

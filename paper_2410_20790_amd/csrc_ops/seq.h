@@ -113,14 +113,27 @@ inline st_status check_seq(const st_seq_desc* d) {
     return bad("unknown data types, or a pair that is not offered");
   if (d->t < 0 || d->b < 0 || d->c < 1)
     return bad("t and b must not be negative, c must be positive");
+  if (d->t > 1 << 30) return bad("t must not lie above 2^30");
   if ((int64_t)d->b * d->c >= (int64_t)1 << 31)
     return bad("b * c must lie below 2^31");
+  if (!aligned(d->lengths, 4)) return bad("lengths is misaligned");
+  return ST_OK;
+}
+// Float arrays and tensors of `es` bytes that may be absent.
+inline st_status check_addresses(std::initializer_list<const void*> floats,
+                                 std::initializer_list<const void*> others,
+                                 int es) {
+  for (const void* p : floats)
+    if (!aligned(p, 4)) return bad("an array of floats is misaligned");
+  for (const void* p : others)
+    if (!aligned(p, es)) return bad("a window is misaligned");
   return ST_OK;
 }
 inline st_status check_ref(const st_seq_desc& d, const st_seq_ref* r,
-                           bool out, const char* name) {
+                           int es, bool out, const char* name) {
   if (!r || (!r->data && !empty(d)))
     return bad(std::string(name) + " is NULL");
+  if (!aligned(r->data, es)) return bad(std::string(name) + " is misaligned");
   if (r->stride_t < 0 || r->stride_b < 0)
     return bad(std::string(name) + " has a negative stride");
   if (out && !empty(d)) {

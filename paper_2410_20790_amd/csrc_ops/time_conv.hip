@@ -209,11 +209,17 @@ extern "C" st_status st_time_conv(const st_seq_desc* d, int32_t taps,
                                   uint64_t ws_bytes, void* stream) {
   return guarded([&]() -> st_status {
     if (const st_status s = check_conv(d, taps, act); s != ST_OK) return s;
-    if (const st_status s = check_ref(*d, x, false, "x"); s != ST_OK) return s;
-    if (const st_status s = check_ref(*d, y, true, "y"); s != ST_OK) return s;
-    if (!weight) return bad("weight is NULL");
-    if (const st_status s = check_ws(0, ws, ws_bytes); s != ST_OK) return s;
     const int es = esize(d->dtype), eo = esize(d->out_dtype);
+    if (const st_status s = check_ref(*d, x, es, false, "x"); s != ST_OK)
+      return s;
+    if (const st_status s = check_ref(*d, y, eo, true, "y"); s != ST_OK)
+      return s;
+    if (!weight) return bad("weight is NULL");
+    if (const st_status s = check_addresses({weight, bias},
+                                            {window, window_out}, es);
+        s != ST_OK)
+      return s;
+    if (const st_status s = check_ws(0, ws, ws_bytes); s != ST_OK) return s;
     const int64_t wb = (int64_t)(taps - 1) * d->b * d->c * es;
     const Span sx = ref_span(*d, x, es), sy = ref_span(*d, y, eo),
                swo = span_of(window_out, wb), sw = span_of(window, wb),
@@ -259,17 +265,23 @@ extern "C" st_status st_time_conv_backward(
     void* stream) {
   return guarded([&]() -> st_status {
     if (const st_status s = check_conv(d, taps, act); s != ST_OK) return s;
-    if (const st_status s = check_ref(*d, dy, false, "dy"); s != ST_OK)
+    const int es = esize(d->dtype), eo = esize(d->out_dtype);
+    if (const st_status s = check_ref(*d, dy, eo, false, "dy"); s != ST_OK)
       return s;
-    if (const st_status s = check_ref(*d, x, false, "x"); s != ST_OK) return s;
+    if (const st_status s = check_ref(*d, x, es, false, "x"); s != ST_OK)
+      return s;
     if (dx)
-      if (const st_status s = check_ref(*d, dx, true, "dx"); s != ST_OK)
+      if (const st_status s = check_ref(*d, dx, es, true, "dx"); s != ST_OK)
         return s;
     if (!weight) return bad("weight is NULL");
+    if (const st_status s = check_addresses(
+            {weight, bias, dweight, dbias}, {window, dwindow_out, dwindow},
+            es);
+        s != ST_OK)
+      return s;
     if (const st_status s = check_ws(conv_space(*d, taps, true), ws, ws_bytes);
         s != ST_OK)
       return s;
-    const int es = esize(d->dtype), eo = esize(d->out_dtype);
     const int64_t wb = (int64_t)(taps - 1) * d->b * d->c * es;
     const int64_t kb = (int64_t)taps * d->c * 4, cb = d->c * 4ll;
     if (any_hit({ref_span(*d, dx, es), span_of(dweight, kb),

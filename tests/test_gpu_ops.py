@@ -169,6 +169,8 @@ def axes(kind, t, b, seed=20):
             ln[1] = 0
         if b > 2:
             ln[2] = t + 5      # counts as t
+        if b > 3:
+            ln[3] = -7         # counts as none
     if "r" in kind:
         rs = (g.random((t, b)) < 0.2).astype(np.uint8) * 3
     return ln, rs, "b" in kind
@@ -380,6 +382,36 @@ def test_reset_stops_what_is_not_finite():
         p = ops.time_conv(v, w, reset=reset)[0]
         q = ops.time_conv(x2, w, reset=reset)[0]
         assert torch.equal(p[at:], q[at:]) and torch.isnan(q[at - 1]).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Steps, rows and images more than 2^31 elements apart, forward and
+    backward, short rows and rows split along time."""
+    say("[gpu] offsets beyond 32 bits")
+    far = 2 ** 31 + 24
+    big = torch.empty(2 * far + 4096, dtype=BF16, device="cuda")
+    for shape, stride in (((3, 2, 8), (far, 40, 1)), ((5, 3, 7),
+                                                      (31, far, 1)),
+                          ((200, 2, 8), (10, far, 1))):
+        x = big.as_strided(shape, stride)
+        x.copy_(rnd(150, *shape, dtype=BF16))
+        scan_both(x, x, x, None, BF16, "lr", f"far {shape}")
+        w = rnd(151, 4, shape[2])
+        y, _ = ops.time_conv(x, w, act=2, reverse=True)
+        check(y, *R.time_conv(f64(x), f64(w), None, R.SILU,
+                              reverse=True)["y"], "far conv")
+        got = ops.time_conv_backward(y, x, w, act=2, out=None)
+        want = R.time_conv_backward(f64(y), f64(x), f64(w), None, R.SILU)
+        check(got[0], *want["dx"], "far conv dx")
+    for shape, stride in (((2, 3, 5, 16), (far, 160, 20, 1)),
+                          ((2, 2, 70, 8), (800, far, 9, 1))):
+        x = big.as_strided(shape, stride)
+        x.copy_(rnd(152, *shape, dtype=BF16))
+        norm_both(x, 2, None, None, R.SILU, BF16, what="far")
+    out = big.as_strided((2, 3, 8), (far, 40, 1))
+    x = rnd(153, 2, 3, 8, dtype=BF16)
+    y, _ = ops.gated_scan(x, x, out=out)
+    check(y, *R.gated_scan(f64(x), f64(x), None)["y"], "far output")
 
 
 def test_sequence_shared_inputs():

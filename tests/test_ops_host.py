@@ -121,7 +121,8 @@ def scan(d=None, v=None, f=None, o=None, h=None, y=None, ho=None, st=None,
 @pytest.mark.parametrize("kw,word", [
     (dict(dtype=5), "types"), (dict(dtype=2, out_dtype=1), "types"),
     (dict(t=-1), "negative"), (dict(b=-1), "negative"),
-    (dict(c=0), "positive"), (dict(b=1 << 20, c=1 << 11), "2^31")])
+    (dict(c=0), "positive"), (dict(b=1 << 20, c=1 << 11), "2^31"),
+    (dict(t=(1 << 30) + 1), "2^30"), (dict(lengths=A + 2), "misaligned")])
 def test_sequence_descriptors(call, kw, word):
     refused(BAD, word, call, seq_desc(**kw))
     for fn in (lambda d: B.st_time_conv_workspace(d, 3, 1),
@@ -192,6 +193,31 @@ def test_scan_refusals():
             df=sref(4 * A + 68, 72, 24))
     refused(BAD, "overlaps", back, dv=sref(4 * A, 72, 24),
             df=sref(4 * A + 32, 144, 24))
+
+
+def test_misaligned_addresses():
+    """Addresses between two elements are refused, in every place."""
+    refused(BAD, "x is misaligned", norm, x=mref(A + 2))
+    refused(BAD, "y is misaligned", norm, norm_desc(out_dtype=1),
+            y=mref(2 * A + 1))
+    refused(BAD, "misaligned", norm, gamma=A + 1)
+    refused(BAD, "misaligned", norm, mean=3 * A + 2, rstd=4 * A)
+    refused(BAD, "x is misaligned", conv, x=sref(A + 1))
+    refused(BAD, "misaligned", conv, w=3 * A + 1)
+    refused(BAD, "window", conv, window=5 * A + 2)
+    refused(BAD, "window", conv, wo=5 * A + 1)
+    refused(BAD, "f is misaligned", scan, f=sref(2 * A + 3))
+    refused(BAD, "y is misaligned", scan, seq_desc(out_dtype=2),
+            y=sref(3 * A + 1))
+    refused(BAD, "misaligned", scan, ho=4 * A + 2)
+    refused(BAD, "misaligned", B.st_gated_scan_backward, seq_desc(), sref(A),
+            sref(2 * A), sref(3 * A), None, 6 * A, None, sref(4 * A + 2),
+            sref(5 * A), None)
+    refused(BAD, "misaligned", B.st_group_norm_backward, norm_desc(),
+            mref(A), mref(2 * A), 3 * A, 4 * A, None, None, mref(7 * A),
+            5 * A + 2)
+    refused(BAD, "misaligned", B.st_time_conv_backward, seq_desc(), 3, 0,
+            sref(A), sref(2 * A), 3 * A, None, None, 5 * A + 2, None)
 
 
 def test_exported_constants():
