@@ -458,7 +458,7 @@ void split_for(const st_norm_desc& d, NormGeom& g, bool backward) {
 struct NormSpace {
   size_t part = 0, bases = 0, chpart = 0, bytes = 0;
 };
-NormSpace space_of(const NormGeom& g, bool backward) {
+NormSpace space_of(const NormGeom& g, bool backward, int held) {
   NormSpace s;
   size_t top = 0;
   auto take = [&](int64_t floats) {
@@ -466,11 +466,12 @@ NormSpace space_of(const NormGeom& g, bool backward) {
     top += (size_t)round_up(floats * 4, (int64_t)kAlign);
     return at;
   };
-  s.part = take((int64_t)g.n * g.groups * g.slabs * g.cparts *
-                (backward ? 2 : 3));
+  if (!held)
+    s.part = take((int64_t)g.n * g.groups * g.slabs * g.cparts *
+                  (backward ? 2 : 3));
   if (backward)
     s.chpart = take((int64_t)g.n * g.slabs * g.c * 2);
-  else
+  else if (!held)
     s.bases = take((int64_t)g.n * g.groups);
   s.bytes = top;
   return s;
@@ -587,8 +588,9 @@ st_status workspace_of(const st_norm_desc* d, int32_t backward,
   for (int v = 8; v >= 1 && d->n > 0; v /= 2) {
     NormGeom g;
     if (!geom(*d, v, g)) continue;
-    split_for(*d, g, backward != 0);
-    *bytes = std::max<uint64_t>(*bytes, space_of(g, backward != 0).bytes);
+    const int held = hold_or_split(*d, g, backward != 0);
+    *bytes =
+        std::max<uint64_t>(*bytes, space_of(g, backward != 0, held).bytes);
   }
   return ST_OK;
 }
@@ -679,7 +681,7 @@ extern "C" st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
     a.g = pick(*d, {{x, es}, {y, eo}});
     const int held = hold_or_split(*d, a.g, false);
     a.act = d->act;
-    const NormSpace sp = space_of(a.g, false);
+    const NormSpace sp = space_of(a.g, false, held);
     char* w = (char*)ws;
     a.x = map_of(*d, *x, a.g);
     a.y = map_of(*d, *y, a.g);
@@ -757,7 +759,7 @@ extern "C" st_status st_group_norm_backward(
     (void)hipGetLastError();
     a.g = pick(*d, {{x, es}, {dy, eo}, {dx, es}});
     const int held = hold_or_split(*d, a.g, true);
-    const NormSpace sp = space_of(a.g, true);
+    const NormSpace sp = space_of(a.g, true, held);
     char* w = (char*)ws;
     a.x = map_of(*d, *x, a.g);
     a.dy = map_of(*d, *dy, a.g);

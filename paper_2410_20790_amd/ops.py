@@ -49,9 +49,12 @@ def _plain(x, shape, dtype, device, name):
     """Address of a contiguous tensor that may be absent."""
     if x is None:
         return None
-    if (not isinstance(x, torch.Tensor) or x.dtype != dtype
-            or x.shape != shape or x.device != device
-            or not x.is_contiguous()):
+    try:
+        good = (x.shape == shape and x.dtype is dtype and x.device == device
+                and x.is_contiguous())
+    except AttributeError:
+        good = False
+    if not good:
         raise _mismatch(name, shape, dtype, device, True)
     return x.data_ptr()
 
@@ -109,11 +112,14 @@ _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
 
 def _map(x, shape, device, name, dtype=None):
     """Reference of a channels-last map of `shape` ([n, ..., c])."""
-    if (not isinstance(x, torch.Tensor) or x.shape != shape
-            or x.device != device
-            or (dtype is not None and x.dtype != dtype)):
+    try:
+        good = (x.shape == shape and x.device == device
+                and (dtype is None or x.dtype is dtype))
+        st = x.stride()
+    except AttributeError:
+        good = False
+    if not good:
         raise _mismatch(name, shape, dtype, device)
-    st = x.stride()
     if st[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name}: channels must be adjacent")
     if len(shape) == 4:
@@ -144,9 +150,9 @@ def group_norm(x, groups, gamma=None, beta=None, act=0, eps=1e-5,
     xr = _map(x, x.shape, dev, "x")
     y = x.new_empty(x.shape, dtype=dt) if out is None else out
     yr = _map(y, x.shape, dev, "out")
-    stats = x.new_empty((2, x.shape[0], groups), dtype=torch.float32)
-    mean, rstd = stats.unbind(0)
     n = B.st_group_norm_workspace(d, 0)
+    stats = x.new_empty((2, d.n, groups), dtype=torch.float32)
+    mean, rstd = stats.unbind(0)
     ws, wp = _workspace(x, n)
     with _On(dev) as stream:
         B.st_group_norm(d, xr, g, b, yr, mean.data_ptr(), rstd.data_ptr(),
@@ -189,11 +195,14 @@ def group_norm_backward(dy, x, groups, mean, rstd, gamma=None, beta=None,
 
 def _seq(x, shape, device, name, dtype=None):
     """Reference of a sequence tensor of `shape` ([t, b, c])."""
-    if (not isinstance(x, torch.Tensor) or x.shape != shape
-            or x.device != device
-            or (dtype is not None and x.dtype != dtype)):
+    try:
+        good = (x.shape == shape and x.device == device
+                and (dtype is None or x.dtype is dtype))
+        st = x.stride()
+    except AttributeError:
+        good = False
+    if not good:
         raise _mismatch(name, shape, dtype, device)
-    st = x.stride()
     if st[2] != 1 and shape[2] != 1:
         raise ValueError(f"{name}: channels must be adjacent")
     return B.st_seq_ref(x.data_ptr(), st[0], st[1])
@@ -230,11 +239,16 @@ def time_conv(x, weight, bias=None, act=0, window=None, lengths=None,
     bp = _plain(bias, (c,), torch.float32, dev, "bias")
     win = _plain(window, (k - 1, b, c), x.dtype, dev, "window")
     xr = _seq(x, x.shape, dev, "x")
-    y = x.new_empty(x.shape, dtype=dt) if out is None else out
-    yr = _seq(y, x.shape, dev, "out")
+    if out is None:
+        y = x.new_empty((t, b, c), dtype=dt)
+        yr = B.st_seq_ref(y.data_ptr(), b * c, c)
+    else:
+        y, yr = out, _seq(out, x.shape, dev, "out")
     if window_out is None:
         window_out = x.new_empty((k - 1, b, c))
-    wo = _plain(window_out, (k - 1, b, c), x.dtype, dev, "window_out")
+        wo = window_out.data_ptr()
+    else:
+        wo = _plain(window_out, (k - 1, b, c), x.dtype, dev, "window_out")
     with _On(dev) as stream:
         B.st_time_conv(d, k, act, xr, w, bp, win, yr, wo, None, 0, stream)
     return y, window_out
@@ -297,11 +311,16 @@ def gated_scan(v, f, o=None, h=None, lengths=None, reset=None, reverse=False,
     fr = _seq(f, v.shape, dev, "f", v.dtype)
     orf = None if o is None else _seq(o, v.shape, dev, "o", v.dtype)
     hp = _plain(h, (b, c), torch.float32, dev, "h")
-    y = v.new_empty(v.shape, dtype=dt) if out is None else out
-    yr = _seq(y, v.shape, dev, "out")
+    if out is None:
+        y = v.new_empty((t, b, c), dtype=dt)
+        yr = B.st_seq_ref(y.data_ptr(), b * c, c)
+    else:
+        y, yr = out, _seq(out, v.shape, dev, "out")
     if h_out is None:
         h_out = v.new_empty((b, c), dtype=torch.float32)
-    ho = _plain(h_out, (b, c), torch.float32, dev, "h_out")
+        ho = h_out.data_ptr()
+    else:
+        ho = _plain(h_out, (b, c), torch.float32, dev, "h_out")
     states = kept_states(t, b, c, dev) if save else None
     n = B.st_gated_scan_workspace(d, 0)
     ws, wp = _workspace(v, n)

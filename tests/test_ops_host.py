@@ -66,8 +66,15 @@ def test_norm_maps_and_memory():
     refused(BAD, "overlaps", norm, gamma=2 * A)
     refused(BAD, "overlaps", norm, ws=2 * A)
     refused(BAD, "aligned", norm, ws=16 * A + 8)
-    refused(BAD, "workspace is NULL", norm, ws=None)
-    refused(SMALL, "small", norm, n=8)
+    # a map of this size is summed up in parts
+    large = dict(d=norm_desc(n=1, h=512, w=512), x=mref(A, 0, 4096, 8),
+                 y=mref(32 * A, 0, 4096, 8), ws=64 * A)
+    need = B.st_group_norm_workspace(large["d"], 0)
+    assert need > 0
+    refused(BAD, "workspace is NULL", norm, **dict(large, ws=None))
+    refused(SMALL, "small", norm, **large, n=need - 1)
+    refused(BAD, "overlaps", norm, **dict(large, ws=33 * A))
+    assert B.st_group_norm_workspace(norm_desc(), 0) == 0
     # types differ: not in place
     refused(BAD, "overlaps", norm, norm_desc(out_dtype=2), y=mref(A))
     assert B.library().st_group_norm(None, None, None, None, None, None, None,
