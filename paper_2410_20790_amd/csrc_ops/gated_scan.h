@@ -23,6 +23,7 @@ struct ScanArgs {
   int tiles, group;                // tiles of a row, tiles of a group
   void* ends;                      // the ticket, then words: tiles, groups
   int narrow;                      // 32-bit offsets within one time
+  int stream;                      // inputs larger than the caches
 };
 constexpr int kHeadWords = 2;
 
@@ -285,8 +286,13 @@ __device__ __forceinline__ void load_steps(const SeqTensor& x, const Whole& w,
                                            Pack<T, V>* out) {
   if (w.on) {
     const WaveWalk<const T> p(x, w.t, w.dir, b, ch);
+    if (a.stream) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) out[k] = load_pack<T, V>(p.at(k));
+      for (int k = 0; k < N; ++k) out[k] = stream_pack<T, V>(p.at(k));
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) out[k] = load_pack<T, V>(p.at(k));
+    }
   } else {
     Walk<const T> p(x, r, b, ch, s0);
 #pragma unroll

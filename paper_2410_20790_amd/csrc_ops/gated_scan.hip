@@ -252,6 +252,14 @@ constexpr int64_t kMaxBlocks = 1 << 22;
 
 constexpr int kTile = kSplit * kWaves, kGradTile = kSplit * kGradWaves;
 
+// Inputs that the last-level cache cannot hold are read past its reuse order:
+// 9 steps of 2048 rows of 2048 channels f32 106 us (125); a chunk that it
+// does hold would lose, 82 MB 28 us for 25.
+constexpr int64_t kCacheBytes = 256 << 20;
+int streamed(const st_seq_desc& d, int64_t bytes_of_a_channel) {
+  return (int64_t)d.t * d.b * d.c * bytes_of_a_channel > kCacheBytes;
+}
+
 struct ScanCut {
   bool split = false;
   int cols = 0, tiles = 0, group = 0;
@@ -387,6 +395,7 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.f = tensor_of(f);
     a.o = tensor_of(o);
     a.y = tensor_of(y);
+    a.stream = streamed(*d, (o ? 3 : 2) * es);
     a.narrow = narrow(*d, v, es) && narrow(*d, f, es) && narrow(*d, o, es) &&
                narrow(*d, y, eo);
     a.h = h;
@@ -465,6 +474,7 @@ extern "C" st_status st_gated_scan_backward(
     a.dv = tensor_of(dv);
     a.df = tensor_of(df);
     a.d_o = tensor_of(d_o);
+    a.stream = streamed(*d, (o ? 3 : 2) * es + eo);
     a.narrow = narrow(*d, dy, eo);
     for (const st_seq_ref* r : {v, f, o, dv, df, d_o})
       a.narrow = a.narrow && narrow(*d, r, es);
