@@ -329,7 +329,11 @@ __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
 }
 
 // Launches (defined beside their kernels).  Rows split along time: blocks of
-// kWaves (backward: kGradWaves) waves.
+// kWaves (backward: kGradWaves) waves, one channel to a lane.  36001 steps of
+// 512 channels bf16, forward: 58 us; 82 with 4 waves, 57 with 16 (shorter rows
+// lose: 300 steps of 30 rows of 1023 channels 38 for 36); two channels to a
+// lane and half the steps 68.  Backward, 4099 steps of 8 rows: 77; 86 with 8
+// waves (a block's registers leave no room for a second beside it).
 constexpr int kWaves = 8, kGradWaves = 4;
 void launch_scan(const ScanArgs& a, int dtype, int out_dtype, int vec,
                  bool split, hipStream_t q);

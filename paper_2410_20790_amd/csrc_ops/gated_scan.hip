@@ -242,12 +242,22 @@ void with_scan(int v, bool gate, F&& f) {
     go(Int<1>{});
 }
 
-// Which rows are split along time: those of more than 64 steps (a chunk's
-// frames, 32 at most, are walked one after another, as they are taken one by
-// one: the same bits) of which there are too few to fill the device, a lane
-// each.
-constexpr int kSerialSteps = 64;
+// Which rows are split along time: those of more than 32 steps (a chunk's
+// frames, so many at most, are walked one after another, as they are taken one
+// by one: the same bits) of which there are too few to fill the device, a wave
+// for each 64 channels.  What fills it, measured on both sides (us, split and
+// walked, bf16, rows of 512 channels unless said):
+//   forward   1000 steps, 150 rows 177 and 246, 300 rows 340 and 296;
+//             100 steps, 300 rows of 256 channels 21 and 26
+//   backward  1000 steps, 150 rows 281 and 379, 300 rows 547 and 690;
+//             300 steps, 600 rows 348 and 349; 100 steps of 256 channels,
+//             300 rows 46 and 36; 100 steps of 8 rows 12 and 23
+constexpr int kSerialSteps = 32, kShortSteps = 128;
 constexpr int64_t kFillWaves = 2048;    // eight to a CU
+int64_t split_waves(const st_seq_desc& d, bool backward) {
+  if (!backward) return kFillWaves;
+  return d.t > kShortSteps ? 2 * kFillWaves : kFillWaves / 2;
+}
 constexpr int64_t kMaxBlocks = 1 << 22;
 
 constexpr int kTile = kSplit * kWaves, kGradTile = kSplit * kGradWaves;
@@ -265,10 +275,12 @@ struct ScanCut {
   int cols = 0, tiles = 0, group = 0;
   uint64_t words = 0;
 };
-ScanCut cut_of(const st_seq_desc& d, int steps) {
+ScanCut cut_of(const st_seq_desc& d, bool backward) {
+  const int steps = backward ? kGradTile : kTile;
   ScanCut c;
   const int64_t cols = ceil_div((int64_t)d.b * d.c, 64);
-  if (d.t <= kSerialSteps || cols >= kFillWaves) return c;
+  if (d.t <= kSerialSteps || cols >= split_waves(d, backward))
+    return c;
   // (as many blocks as a launch may have; beyond that, rows are walked)
   if (cols * ceil_div(d.t, steps) > kMaxBlocks) return c;
   c.split = true;
@@ -285,7 +297,7 @@ ScanCut cut_of(const st_seq_desc& d, int steps) {
 
 uint64_t scan_space(const st_seq_desc& d, bool backward) {
   if (empty(d)) return 0;
-  const uint64_t words = cut_of(d, backward ? kGradTile : kTile).words;
+  const uint64_t words = cut_of(d, backward).words;
   return (words * 8 + 15) / 16 * 16;
 }
 
@@ -402,7 +414,7 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.h_out = h_out;
     a.states = states;
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, kTile);
+    const ScanCut cut = cut_of(*d, false);
     vec = cut.split ? 1 : lane_vec(*d, vec);
     a.cv = d->c / vec;
     a.lanes = (int64_t)d->b * a.cv;
@@ -482,7 +494,7 @@ extern "C" st_status st_gated_scan_backward(
     a.h_out = dh;
     a.states = const_cast<float*>(states);
     hipStream_t q = (hipStream_t)stream;
-    const ScanCut cut = cut_of(*d, kGradTile);
+    const ScanCut cut = cut_of(*d, true);
     a.cv = d->c;
     a.lanes = (int64_t)d->b * d->c;
     take_cut(a, cut, ws, q);

@@ -223,8 +223,8 @@ struct Entries {
 
 // -------------------------------------------------------------- host side
 
-// The held kernels: threads of a block, vectors a thread holds (of x and dy
-// together in the backward pass).
+// The held kernels: threads of a block, sites a thread holds (backward, where
+// it holds x and dy: half as many in the larger blocks).
 constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kHeld = 8;
 

@@ -106,16 +106,16 @@ __device__ __forceinline__ void block_moments(const NormGeom& g,
   const int wide = !WHOLE ? g.cpg : g.cparts == 1 ? g.unit_vec : p.nvec;
   const int lanes = lanes_per_group(TH, p.ng), in = tid & (lanes - 1);
   const Entries first(in, lanes, wide);
+  const float n = (float)(p.s1 - p.s0) *
+                  (float)(g.cparts == 1 ? g.cpg : p.nvec * V);
   for (int j = tid / lanes; j < p.ng; j += TH / lanes) {
-    float n = 0.f, q = 0.f;
+    float q = 0.f;
     double s = 0;   // (its values need not be near zero)
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
-      n += sc[at];
       s += (double)sc[at] * sm[at];
     }
-    n = lanes_sum(n, lanes);
-    const float mean = (float)(lanes_sum(s, lanes) / n);
+    const float mean = (float)lanes_sum(s, lanes) / n;
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
       const float d = sm[at] - mean;
@@ -347,14 +347,22 @@ __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
 
 // -------------------------------------------------------------- host side
 
-constexpr int kHeldBlocks = 256;      // one to a CU
-
-constexpr int kTargetBlocks = 1024;   // four of 256 threads to a CU
+// Rules of the cut, each with what it measured (us, in a replayed graph).
+// Held blocks take more groups, for whole cache lines, while there is one to a
+// CU: 32 images of 8x8x320 f32 7.4 (8.4 with two to a CU).
+constexpr int kHeldBlocks = 256;
+// Blocks of 256 threads that a batch of images is cut into: four to a CU;
+// 4x61x67x513 f16 29 (34 with eight), others within 1%.
+constexpr int kTargetBlocks = 1024;
 constexpr int kMaxEntries = 4096;     // parts of all groups a block joins
 constexpr int kMinSites = 16;         // sites a thread has at least
-constexpr int kLine = 256;            // bytes of a site to a block
-// Bytes of the images of a batch: what is read again after one more batch
-// was read and one written must be in the last-level cache still (256 MiB).
+// Bytes of a site to a block, two cache lines: 9x256x512x256 bf16 357 (368
+// with four lines, 353 with one, which loses where they are streamed out).
+constexpr int kLine = 256;
+// Bytes of the images of a batch, read by one launch and again by the next,
+// which also writes as many, while the last-level cache holds 256 MiB:
+// 9x256x512x256 bf16 329 in six launches (357 in batches of 48 MiB, ten
+// launches; 339 in one batch).
 constexpr int64_t kBatchBytes = 144 << 20;
 
 // The cut for vectors of v channels; false where v does not suit the groups.
@@ -568,9 +576,8 @@ NormMap map_of(const st_norm_desc& d, const st_map_ref& m,
   return r;
 }
 // The threads of the blocks that hold the image's groups (of x and dy in the
-// backward pass), or 0 and a cut into site ranges.  (A block that holds up to
-// 128 KiB takes about as long as a second launch would; larger groups go over
-// all CUs in ranges.)
+// backward pass), or 0 and a cut into site ranges.  (8x47x78x512 f16 22 us
+// held, 26 in ranges; 4x64x64x256 f16 15 and 17; 32x8x8x320 f32 8 and 14.)
 int hold_or_split(const st_norm_desc& d, NormGeom& g, bool backward) {
   if (hold(g, kFewThreads, kHeld)) return kFewThreads;
   if (hold(g, kManyThreads, backward ? kHeld / 2 : kHeld))
