@@ -439,7 +439,7 @@ typedef struct st_map_ref {
 } st_map_ref;
 
 /* Group norm with an activation.  groups divides c.  act: ST_ACT_*.  n may
- * be 0; h, w, c at least 1; n * c below 2^31. */
+ * be 0; h, w, c at least 1; n * c below 2^31, h * w * c below 2^40. */
 typedef struct st_norm_desc {
   int32_t dtype, out_dtype;
   int32_t n, h, w, c, groups, act;

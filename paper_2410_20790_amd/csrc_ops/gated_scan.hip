@@ -267,7 +267,7 @@ constexpr int kTile = kSplit * kWaves, kGradTile = kSplit * kGradWaves;
 // does hold would lose, 82 MB 28 us for 25.
 constexpr int64_t kCacheBytes = 256 << 20;
 int streamed(const st_seq_desc& d, int64_t bytes_of_a_channel) {
-  return (int64_t)d.t * d.b * d.c * bytes_of_a_channel > kCacheBytes;
+  return (int64_t)d.t * d.b * d.c > kCacheBytes / bytes_of_a_channel;
 }
 
 struct ScanCut {

@@ -493,6 +493,8 @@ st_status check_desc(const st_norm_desc* d) {
     return bad("the map's sizes must be positive (n may be 0)");
   if ((int64_t)d->n * d->c >= (int64_t)1 << 31)
     return bad("n * c must lie below 2^31");
+  if ((int64_t)d->h * d->w >= ((int64_t)1 << 40) / d->c)
+    return bad("h * w * c must lie below 2^40");
   if (d->groups < 1 || d->c % d->groups)
     return bad("groups must divide the channels");
   if (!act_known(d->act)) return bad("unknown activation");

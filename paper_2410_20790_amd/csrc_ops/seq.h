@@ -153,11 +153,16 @@ inline Span ref_span(const st_seq_desc& d, const st_seq_ref* r, int es) {
                            d.c) * es);
 }
 // Two tensors of one type whose spans cross but whose elements do not: equal
-// strides, and channels side by side (slices of one wider tensor).
+// strides, and channels side by side (slices of one wider tensor, whose outer
+// axis steps over the inner one whole).
 inline bool side_by_side(const st_seq_desc& d, const st_seq_ref& a,
                          const st_seq_ref& b, int es) {
   if ((d.t > 1 && a.stride_t != b.stride_t) ||
       (d.b > 1 && a.stride_b != b.stride_b))
+    return false;
+  if (d.t > 1 && d.b > 1 &&
+      (a.stride_t <= a.stride_b ? a.stride_b < a.stride_t * d.t
+                                : a.stride_t < a.stride_b * d.b))
     return false;
   const int64_t bytes = std::abs((const char*)a.data - (const char*)b.data);
   int64_t room = INT64_MAX;   // the narrowest step of the two axes

@@ -71,7 +71,8 @@ class RecurrentHead:
         if feats.dim() != 5 or feats.shape[-1] != 3 * c:
             raise ValueError(f"feats must be [t, n, h, w, {3 * c}]")
         # one row for each site; views of the encoder's maps
-        seq = feats.reshape(feats.shape[0], -1, 3 * c)
+        t, n, h, w, _ = feats.shape
+        seq = feats.reshape(t, n * h * w, 3 * c)
         return seq[..., :c], seq[..., c:2 * c], seq[..., 2 * c:]
 
     def forward(self, feats, state: HeadState, reset=None, save=False):

@@ -248,3 +248,22 @@ def test_tensors_on_the_host_are_refused():
                  lambda: ops.gated_scan(x[0], x[0])):
         with pytest.raises(ValueError, match="device tensor"):
             call()
+
+
+def test_scan_gradients_that_cross_in_the_next_step():
+    """Slices whose steps are narrower than all their rows side by side: the
+    last row of one lies where the next step's first row of the other does."""
+    d = seq_desc(t=2, b=2, c=4)
+    for axes in ((16, 12), (12, 16)):
+        refused(BAD, "overlaps", B.st_gated_scan_backward, d, sref(A),
+                sref(2 * A), sref(3 * A), None, 6 * A, None,
+                sref(4 * A, *axes), sref(4 * A + 16, *axes), None)
+
+
+def test_maps_larger_than_any_memory():
+    """Sizes whose product passes 64 bits are refused, not computed with."""
+    for h, w, c in ((1 << 30, 1 << 30, 8), (1 << 30, 1 << 30, 4),
+                    ((1 << 31) - 1, (1 << 31) - 1, 1), (1 << 20, 1 << 10, 2048)):
+        d = norm_desc(n=1, h=h, w=w, c=c, groups=1)
+        for back in (0, 1):
+            refused(BAD, "2^40", B.st_group_norm_workspace, d, back)
