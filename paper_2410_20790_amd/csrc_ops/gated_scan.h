@@ -32,8 +32,8 @@ constexpr int kHeadWords = 2;
 // Few rows and channels, many steps: a thread for each would leave the device
 // idle.  h_s = a_s h_{s-1} + u_s joins: a run of steps acts as h -> A h + H
 // with A the product of its a (d -> A d + D for the gradient, whose order is
-// the reverse).  A block takes a tile: 64 lanes (V adjacent channels of a row
-// each) over W waves, a wave kSplit steps of every lane.  Gates and inputs of
+// the reverse).  A block takes a tile: 64 lanes (a channel of a row each) over
+// W waves, a wave kSplit steps of every lane.  Gates and inputs of
 // these steps stay in registers, so that all is read once and every gate
 // computed once; the tile's (A, H) is published, those of the tiles before it
 // are folded, and the steps are run from the state that enters.
@@ -56,23 +56,14 @@ __device__ __forceinline__ bool is_cut(float A) {
 }
 
 // (A, H), then (x, y): the steps of (x, y) run after those of (A, H).
-template <int V>
-__device__ __forceinline__ void then(float* A, float* H, const float* x,
-                                     const float* y) {
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const bool cut = is_cut(x[e]);
-    H[e] = cut ? y[e] : __builtin_fmaf(x[e], H[e], y[e]);
-    A[e] = cut ? x[e] : A[e] * x[e];
-  }
+__device__ __forceinline__ void then(float& A, float& H, float x, float y) {
+  const bool cut = is_cut(x);
+  H = cut ? y : __builtin_fmaf(x, H, y);
+  A = cut ? x : A * x;
 }
-template <int V>
-__device__ __forceinline__ void none(float* A, float* H) {
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    A[e] = 1.f;
-    H[e] = 0.f;
-  }
+// The state after the steps of (A, H), from the state h.
+__device__ __forceinline__ float after(float A, float H, float h) {
+  return is_cut(A) ? H : __builtin_fmaf(A, h, H);
 }
 
 // A published (A, H) of a channel, in one 8-byte word, so that it is whole when
@@ -94,47 +85,33 @@ __device__ __forceinline__ Word peek(const Word* w) {
 struct Ends {
   Word* base;        // of entry 0, this lane
   int64_t plane;     // words of an entry
+  __device__ __forceinline__ Word* at(int64_t i) const {
+    return base + i * plane;
+  }
 };
-template <int V>
-__device__ __forceinline__ void put_entry(const Ends& p, int64_t i,
-                                          const float* A, const float* H) {
-#pragma unroll
-  for (int e = 0; e < V; ++e) publish(p.base + i * p.plane + e, A[e], H[e]);
-}
 // Folds entries [i0, i1) into (A, H), four at a time, waiting for each.
-template <int V>
 __device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
-                                             float* A, float* H) {
-  constexpr int N = 4 / V;
-  const Word* q = p.base + (int64_t)i0 * p.plane;
+                                             float& A, float& H) {
+  constexpr int N = 4;
+  const Word* q = p.at(i0);
   for (int i = i0; i < i1; i += N) {
-    Word w[N][V];
+    Word w[N];
     bool all;
     do {
       all = true;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const Word* x = q + (int64_t)min(k, i1 - 1 - i) * p.plane;
-#pragma unroll
-        for (int e = 0; e < V; ++e) w[k][e] = peek(x + e);
-      }
-#pragma unroll
       for (int k = 0; k < N; ++k)
+        w[k] = peek(q + (int64_t)min(k, i1 - 1 - i) * p.plane);
 #pragma unroll
-        for (int e = 0; e < V; ++e) all = all && (w[k][e] >> 63) != 0;
+      for (int k = 0; k < N; ++k) all = all && (w[k] >> 63) != 0;
       if (!all) __builtin_amdgcn_s_sleep(1);
     } while (!all);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       if (i + k < i1) {
-        float x[V], y[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const uint32_t hi = (uint32_t)(w[k][e] >> 32);
-          x[e] = hi == kCutBits ? kCut : __uint_as_float(hi & 0x7fffffffu);
-          y[e] = __uint_as_float((uint32_t)w[k][e]);
-        }
-        then<V>(A, H, x, y);
+        const uint32_t hi = (uint32_t)(w[k] >> 32);
+        then(A, H, hi == kCutBits ? kCut : __uint_as_float(hi & 0x7fffffffu),
+             __uint_as_float((uint32_t)w[k]));
       }
     }
     q += N * p.plane;
@@ -143,37 +120,32 @@ __device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
 
 // A block's lanes and waves, in running order: wave 0 has the first steps to
 // run (of the backward pass: the row's last).
-template <int V, int W>
+template <int W>
 struct TileShared {
-  float a[W][64 * V], h[W][64 * V];
+  float a[W][64], h[W][64];
   int ticket;
 };
 
 // Joins the waves' (A, H) in LDS: each wave gets what runs before it in `A, H`
 // and every wave the whole in `TA, TH`.
-template <int V, int W>
-__device__ __forceinline__ void join_waves(TileShared<V, W>& sh, int wave,
-                                           float* A, float* H, float* TA,
-                                           float* TH) {
-  const int at = (threadIdx.x & 63) * V;
+template <int W>
+__device__ __forceinline__ void join_waves(TileShared<W>& sh, int wave,
+                                           float& A, float& H, float& TA,
+                                           float& TH) {
+  const int at = threadIdx.x & 63;
   __syncthreads();
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    sh.a[wave][at + e] = A[e];
-    sh.h[wave][at + e] = H[e];
-  }
+  sh.a[wave][at] = A;
+  sh.h[wave][at] = H;
   __syncthreads();
-  none<V>(TA, TH);
+  TA = 1.f;
+  TH = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
     if (w == wave) {
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        A[e] = TA[e];
-        H[e] = TH[e];
-      }
+      A = TA;
+      H = TH;
     }
-    then<V>(TA, TH, &sh.a[w][at], &sh.h[w][at]);
+    then(TA, TH, sh.a[w][at], sh.h[w][at]);
   }
 }
 
@@ -181,59 +153,54 @@ __device__ __forceinline__ void join_waves(TileShared<V, W>& sh, int wave,
 // tiles before it, given the tile's own (TA, TH).  h comes in as the state
 // before the first tile, which only tile 0 has (the row's state may be
 // replaced in place once the last tile has run).
-template <int V, int W>
+template <int W>
 __device__ __forceinline__ void enter_tile(const ScanArgs& a,
-                                           TileShared<V, W>& sh, int k,
-                                           int col, int wave, float* TA,
-                                           float* TH, float* h) {
+                                           TileShared<W>& sh, int k, int col,
+                                           int wave, float TA, float TH,
+                                           float& h) {
   if (a.tiles == 1) return;
   Ends p;
-  p.plane = (int64_t)a.cols * 64 * V;
-  p.base = (Word*)a.ends + kHeadWords +
-           ((int64_t)col * 64 + (threadIdx.x & 63)) * V;
+  p.plane = (int64_t)a.cols * 64;
+  p.base = (Word*)a.ends + kHeadWords + (int64_t)col * 64 +
+           (threadIdx.x & 63);
   if (k == 0) {
     // nothing enters but h: the tile's end is a state
-    if (wave == 0) {
-      float cut[V], end[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        cut[e] = kCut;
-        end[e] = is_cut(TA[e]) ? TH[e] : __builtin_fmaf(TA[e], h[e], TH[e]);
-      }
-      put_entry<V>(p, 0, cut, end);
-    }
+    if (wave == 0) publish(p.at(0), kCut, after(TA, TH, h));
     return;
   }
-  if (wave == 0) put_entry<V>(p, k, TA, TH);
+  if (wave == 0) publish(p.at(k), TA, TH);
   const int g = k / a.group, in = k % a.group;
-  float A[V], H[V], PA[V], PH[V];
+  float A = 1.f, H = 0.f, PA, PH;
   // the tiles of its group before it, a share to each wave
-  none<V>(A, H);
   const int share = (in + W - 1) / W;
   const int g0 = g * a.group;
-  fold_entries<V>(p, g0 + min(wave * share, in),
-                  g0 + min((wave + 1) * share, in), A, H);
-  join_waves<V, W>(sh, wave, A, H, PA, PH);
+  fold_entries(p, g0 + min(wave * share, in), g0 + min((wave + 1) * share, in),
+               A, H);
+  join_waves(sh, wave, A, H, PA, PH);
   if (in == a.group - 1 && wave == 0 && k < a.tiles - 1) {
     // the last of its group publishes the group
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      A[e] = PA[e];
-      H[e] = PH[e];
-    }
-    then<V>(A, H, TA, TH);
-    put_entry<V>(p, (int64_t)a.tiles + g, A, H);
+    A = PA;
+    H = PH;
+    then(A, H, TA, TH);
+    publish(p.at((int64_t)a.tiles + g), A, H);
   }
   // the groups before its own
-  none<V>(A, H);
+  A = 1.f;
+  H = 0.f;
   const int gs = (g + W - 1) / W;
-  fold_entries<V>(p, a.tiles + min(wave * gs, g),
-                  a.tiles + min((wave + 1) * gs, g), A, H);
-  float GA[V], GH[V];
-  join_waves<V, W>(sh, wave, A, H, GA, GH);
-  then<V>(GA, GH, PA, PH);
-#pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = GH[e];
+  fold_entries(p, a.tiles + min(wave * gs, g),
+               a.tiles + min((wave + 1) * gs, g), A, H);
+  float GA, GH;
+  join_waves(sh, wave, A, H, GA, GH);
+  then(GA, GH, PA, PH);
+  h = GH;
+}
+
+// The state before a row's first tile, arrived in all waves of that tile before
+// their first barrier: behind it the tile publishes, and the last tile may
+// write the state's place.
+__device__ __forceinline__ void arrived(float& h) {
+  asm volatile("" : "+v"(h));
 }
 
 struct LaneAt {
@@ -241,20 +208,19 @@ struct LaneAt {
   bool on;          // otherwise a copy of the last lane that stores nothing
   int64_t hc;
 };
-__device__ __forceinline__ LaneAt lane_at(const ScanArgs& a, int col,
-                                          int v) {
+__device__ __forceinline__ LaneAt lane_at(const ScanArgs& a, int col) {
   int64_t lane = (int64_t)col * 64 + (threadIdx.x & 63);
   LaneAt l;
   l.on = lane < a.lanes;
   if (!l.on) lane = a.lanes - 1;
   l.b = (int)(lane / a.cv);
-  l.ch = (int)(lane % a.cv) * v;
+  l.ch = (int)(lane % a.cv);
   l.hc = (int64_t)l.b * a.q.c + l.ch;
   return l;
 }
-template <int V, int W>
+template <int W>
 __device__ __forceinline__ int next_ticket(const ScanArgs& a,
-                                           TileShared<V, W>& sh) {
+                                           TileShared<W>& sh) {
   if (a.tiles == 1) return blockIdx.x;
   if (threadIdx.x == 0)
     sh.ticket = (int)__hip_atomic_fetch_add((unsigned*)a.ends, 1u,

@@ -81,140 +81,97 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
   }
 }
 
-template <typename T, typename O, int V, bool GATE, int W>
+template <typename T, typename O, bool GATE, int W>
 __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
-  __shared__ TileShared<V, W> sh;
-  const int ticket = next_ticket<V, W>(a, sh);
+  __shared__ TileShared<W> sh;
+  const int ticket = next_ticket(a, sh);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int tile = ticket / a.cols, col = ticket % a.cols;
-  const LaneAt l = lane_at(a, col, V);
+  const LaneAt l = lane_at(a, col);
   const Row r = row_of(a.q, l.b);
   const int64_t plane = (int64_t)a.q.b * a.q.c;
   const int s0 = (tile * W + wave) * kSplit;
-  float h[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = tile == 0 && a.h ? a.h[l.hc + e] : 0.f;
+  float h = tile == 0 && a.h ? a.h[l.hc] : 0.f;
   const bool any = __any(s0 < r.len);
   const Whole whole = whole_wave(a, r, s0, kSplit);
-  float keep[kSplit][V], u[kSplit][V];
-  Pack<T, V> io[kSplit];
+  float keep[kSplit], u[kSplit];
+  Pack<T, 1> io[kSplit];
   unsigned cuts = 0;
   bool cutting = false;
-  float A[V], H[V], TA[V], TH[V];
-  none<V>(A, H);
+  float A = 1.f, H = 0.f, TA, TH;
   if (any) {
     cuts = cuts_of<kSplit>(a, r, l.b, s0);
-    Pack<T, V> iv[kSplit], jf[kSplit];
-    load_steps<T, V, kSplit>(a.f, whole, a, r, l.b, l.ch, s0, jf);
-    load_steps<T, V, kSplit>(a.v, whole, a, r, l.b, l.ch, s0, iv);
-    if (GATE) load_steps<T, V, kSplit>(a.o, whole, a, r, l.b, l.ch, s0, io);
+    Pack<T, 1> iv[kSplit], jf[kSplit];
+    load_steps<T, 1, kSplit>(a.f, whole, a, r, l.b, l.ch, s0, jf);
+    load_steps<T, 1, kSplit>(a.v, whole, a, r, l.b, l.ch, s0, iv);
+    if (GATE) load_steps<T, 1, kSplit>(a.o, whole, a, r, l.b, l.ch, s0, io);
 #pragma unroll
     for (int k = 0; k < kSplit; ++k) {
-      float v[V], f[V];
-      unpack<T, V>(iv[k], v);
-      unpack<T, V>(jf[k], f);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float write;
-        sigmoids(f[e], keep[k][e], write);
-        u[k][e] = write * v[e];
-      }
+      float write;
+      sigmoids(to_f(jf[k].e[0]), keep[k], write);
+      u[k] = write * to_f(iv[k].e[0]);
     }
     // steps behind the row's end keep the state, to the bit
     if (!whole.on) {
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          keep[k][e] = s0 + k < r.len ? keep[k][e] : 1.f;
-          u[k][e] = s0 + k < r.len ? u[k][e] : 0.f;
-        }
+      for (int k = 0; k < kSplit; ++k) {
+        keep[k] = s0 + k < r.len ? keep[k] : 1.f;
+        u[k] = s0 + k < r.len ? u[k] : 0.f;
+      }
     }
     cutting = __any(cuts != 0);
     if (cutting) {
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const bool cut = cuts >> k & 1;
-          H[e] = __builtin_fmaf(keep[k][e], cut ? 0.f : H[e], u[k][e]);
-          A[e] = cut ? kCut : A[e] * keep[k][e];
-        }
+      for (int k = 0; k < kSplit; ++k) {
+        const bool cut = cuts >> k & 1;
+        H = __builtin_fmaf(keep[k], cut ? 0.f : H, u[k]);
+        A = cut ? kCut : A * keep[k];
+      }
     } else {
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          H[e] = __builtin_fmaf(keep[k][e], H[e], u[k][e]);
-          A[e] *= keep[k][e];
-        }
+      for (int k = 0; k < kSplit; ++k) {
+        H = __builtin_fmaf(keep[k], H, u[k]);
+        A *= keep[k];
+      }
     }
   }
-  join_waves<V, W>(sh, wave, A, H, TA, TH);
-  float WA[V], WH[V];     // what runs before the wave in its tile
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    WA[e] = A[e];
-    WH[e] = H[e];
-  }
-  enter_tile<V, W>(a, sh, tile, col, wave, TA, TH, h);
-  if (tile == a.tiles - 1 && a.h_out && wave == 0 && l.on) {
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      a.h_out[l.hc + e] =
-          is_cut(TA[e]) ? TH[e] : __builtin_fmaf(TA[e], h[e], TH[e]);
-  }
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    h[e] = is_cut(WA[e]) ? WH[e] : __builtin_fmaf(WA[e], h[e], WH[e]);
+  if (tile == 0) arrived(h);
+  join_waves(sh, wave, A, H, TA, TH);
+  const float WA = A, WH = H;     // what runs before the wave in its tile
+  enter_tile(a, sh, tile, col, wave, TA, TH, h);
+  if (tile == a.tiles - 1 && a.h_out && wave == 0 && l.on)
+    a.h_out[l.hc] = after(TA, TH, h);
+  h = after(WA, WH, h);
   if (!l.on) return;
   if (any) {
-    if (a.states && s0 < r.len)
-      store_pack<float, V>(a.states + (s0 / kStride) * plane + l.hc, h);
-    auto gated = [&](int k, float* y) {
-      float o[V];
-      if (GATE) unpack<T, V>(io[k], o);
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        y[e] = GATE ? h[e] * sigmoid_once(o[e]) : h[e];
+    if (a.states && s0 < r.len) a.states[(s0 / kStride) * plane + l.hc] = h;
+    auto gated = [&](int k) {
+      return GATE ? h * sigmoid_once(to_f(io[k].e[0])) : h;
     };
     if (whole.on && !cutting) {
       const WaveWalk<O> ww(a.y, whole.t, whole.dir, l.b, l.ch);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
-        float y[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          h[e] = __builtin_fmaf(keep[k][e], h[e], u[k][e]);
-        gated(k, y);
-        store_pack<O, V>(ww.at(k), y);
+        h = __builtin_fmaf(keep[k], h, u[k]);
+        *ww.at(k) = from_f<O>(gated(k));
       }
     } else {
       Walk<O> wy(a.y, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         if (s0 + k < r.len) {
-          float y[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            if (cuts >> k & 1) h[e] = 0.f;
-            h[e] = __builtin_fmaf(keep[k][e], h[e], u[k][e]);
-          }
-          gated(k, y);
-          store_pack<O, V>(wy.p, y);
+          if (cuts >> k & 1) h = 0.f;
+          h = __builtin_fmaf(keep[k], h, u[k]);
+          *wy.p = from_f<O>(gated(k));
           wy.next();
         }
       }
     }
   }
-  O* py = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
+  O* y = (O*)a.y.p + (int64_t)l.b * a.y.sb + l.ch;
   const int s1 = min(s0 + kSplit, a.q.t);
-  for (int s = max(s0, r.len); s < s1; ++s) {
-    float z[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) z[e] = 0.f;
-    store_pack<O, V>(py + (int64_t)s * a.y.st, z);
-  }
+  for (int s = max(s0, r.len); s < s1; ++s)
+    y[(int64_t)s * a.y.st] = from_f<O>(0.f);
 }
 
 // Clears the words and the ticket of a launch.
@@ -227,19 +184,20 @@ __global__ __launch_bounds__(256) void k_scan_clear(uint4* w, int64_t n) {
 // -------------------------------------------------------------- host side
 
 template <class F>
-void with_scan(int v, bool gate, F&& f) {
-  auto go = [&](auto vt) {
-    if (gate)
-      f(vt, std::true_type{});
-    else
-      f(vt, std::false_type{});
-  };
-  if (v == 4)
-    go(Int<4>{});
-  else if (v == 2)
-    go(Int<2>{});
+void with_gate(bool gate, F&& f) {
+  if (gate)
+    f(std::true_type{});
   else
-    go(Int<1>{});
+    f(std::false_type{});
+}
+template <class F>
+void with_lane_vec(int v, F&& f) {
+  if (v == 4)
+    f(Int<4>{});
+  else if (v == 2)
+    f(Int<2>{});
+  else
+    f(Int<1>{});
 }
 
 // Which rows are split along time: those of more than 32 steps (a chunk's
@@ -327,16 +285,17 @@ void launch_scan(const ScanArgs& a, int dtype, int out_dtype, int vec,
   with_types(dtype, out_dtype, [&](auto ti, auto to) {
     using T = typename decltype(ti)::type;
     using O = typename decltype(to)::type;
-    with_scan(vec, a.o.p != nullptr, [&](auto vt, auto gt) {
-      constexpr int V = decltype(vt)::value;
+    with_gate(a.o.p != nullptr, [&](auto gt) {
       constexpr bool G = decltype(gt)::value;
-      if (!split)
-        k_scan<T, O, V, G>
-            <<<(unsigned)ceil_div(a.lanes, kScanThreads), kScanThreads, 0,
-               q>>>(a);
-      else if constexpr (V == 1)
-        k_scan_tiles<T, O, V, G, kWaves>
+      if (split)
+        k_scan_tiles<T, O, G, kWaves>
             <<<(unsigned)(a.cols * a.tiles), 64 * kWaves, 0, q>>>(a);
+      else
+        with_lane_vec(vec, [&](auto vt) {
+          k_scan<T, O, decltype(vt)::value, G>
+              <<<(unsigned)ceil_div(a.lanes, kScanThreads), kScanThreads, 0,
+                 q>>>(a);
+        });
     });
   });
 }

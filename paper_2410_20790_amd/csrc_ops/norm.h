@@ -27,7 +27,6 @@ struct NormGeom {
   int cv;              // vectors per site
   int cols, rows;      // vectors and sites a block takes at a time
   int colblocks, kg, cparts, unit_vec;
-  int threads;         // of a block
   int slabs;           // site ranges per image, per column block
   int64_t slab_sites;
   int units;           // slabs * colblocks, of one image

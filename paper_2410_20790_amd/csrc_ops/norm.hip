@@ -387,7 +387,6 @@ bool geom(const st_norm_desc& d, int v, NormGeom& g) {
 // fill whole vectors in each.
 void columns(NormGeom& g, int threads, int units) {
   const int mul = g.v / std::gcd(g.cpg, g.v);
-  g.threads = threads;
   g.unit_vec = g.cpg * mul / g.v;
   if (g.unit_vec <= kMaxCols) {
     const int all = g.groups / mul;

@@ -31,7 +31,6 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
 // The same past the caches' reuse order: for data that is streamed through
 // once.  Whole lines only (a store of part of one costs a read of the rest).
 template <int N> struct Bits;
-template <> struct Bits<1> { typedef uint8_t type; };
 template <> struct Bits<2> { typedef uint16_t type; };
 template <> struct Bits<4> { typedef uint32_t type; };
 template <> struct Bits<8> {
@@ -91,11 +90,6 @@ __device__ __forceinline__ void sigmoids(float x, float& pos, float& neg) {
   const float big = rcp_1to2(1.f + e), small = e * big;
   pos = x >= 0.f ? big : small;
   neg = x >= 0.f ? small : big;
-}
-__device__ __forceinline__ float sigmoid(float x) {
-  float p, n;
-  sigmoids(x, p, n);
-  return p;
 }
 
 // sigmoid(x) where it scales a value once: off by some (4 + 1.25 |x|) 2^-24 of

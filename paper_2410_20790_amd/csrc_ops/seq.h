@@ -45,7 +45,7 @@ __device__ __forceinline__ bool reset_at(const SeqAxes& q, const Row& r,
   return q.reset && q.reset[time_of(r, s) * q.b + b] != 0;
 }
 
-// A row's elements in running order, from step s0 on: advance() goes to the
+// A row's elements in running order, from step s0 on: next() goes to the
 // next step, or stays where the row ends (an address that may be read, time 0
 // of a row of no steps).  One addition per step; the products that a time and
 // its stride make up are formed once.
@@ -62,10 +62,7 @@ struct Walk {
     step = r.dir * x.st;
     left = last - s;
   }
-  __device__ __forceinline__ void advance(int k) {  // from step s0 + k
-    if (k < left) p += step;
-  }
-  __device__ __forceinline__ void next() {          // likewise, one by one
+  __device__ __forceinline__ void next() {
     if (left > 0) {
       p += step;
       --left;
