@@ -22,7 +22,7 @@ struct ScanArgs {
   int cols;                        // blocks of 64 lanes
   int tiles, group;                // tiles of a row, tiles of a group
   void* ends;                      // the ticket, then words: tiles, groups
-  int narrow;                      // 32-bit offsets within one time
+  int narrow;                      // 32-bit offsets (see StepsAt)
   int stream;                      // inputs larger than the caches
 };
 constexpr int kHeadWords = 2;
@@ -229,63 +229,45 @@ __device__ __forceinline__ int next_ticket(const ScanArgs& a,
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(sh.ticket);
 }
-// Whether all lanes of a wave have all of `steps` steps from s0 on, at the same
-// times, and the time of the first.
-struct Whole {
-  bool on;
-  int64_t t;
-  int dir;
-};
-__device__ __forceinline__ Whole whole_wave(const ScanArgs& a, const Row& r,
-                                            int s0, int steps) {
-  Whole w;
-  w.on = a.narrow && !(a.q.lengths && a.q.reverse) &&
-         __all(s0 + steps <= r.len);
-  w.t = a.q.reverse ? a.q.t - 1 - s0 : s0;
-  w.dir = a.q.reverse ? -1 : 1;
-  return w;
-}
-template <typename T, int V, int N>
-__device__ __forceinline__ void load_steps(const SeqTensor& x, const Whole& w,
+// N steps of a tensor from step s0 on; for those that the row does not have,
+// whatever it has last.  whole: all lanes of the wave have all of them.
+template <int N, bool NARROW, typename T, int V>
+__device__ __forceinline__ void load_steps(const SeqTensor& x,
                                            const ScanArgs& a, const Row& r,
-                                           int b, int ch, int s0,
+                                           int b, int ch, int s0, bool whole,
                                            Pack<T, V>* out) {
-  if (w.on) {
-    const WaveWalk<const T> p(x, w.t, w.dir, b, ch);
-    if (a.stream) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) out[k] = stream_pack<T, V>(p.at(k));
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k) out[k] = load_pack<T, V>(p.at(k));
-    }
-  } else {
-    Walk<const T> p(x, r, b, ch, s0);
+  StepsAt<const T, NARROW> p(x, a.q, r, b, ch, s0);
+  if (!whole) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      if (s0 + k < a.q.t) {      // no row is longer
-        out[k] = load_pack<T, V>(p.p);
-        p.next();
-      }
-      // one address at a time, not all of them in registers first
+      out[k] = load_pack<T, V>(p.here());
+      p.next(k);
+      // (keeps these loads apart from those below: the compiler would form all
+      // addresses in registers first and load in one place)
       __builtin_amdgcn_sched_barrier(0);
     }
+  } else if (a.stream) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) out[k] = stream_pack<T, V>(p.at(k));
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) out[k] = load_pack<T, V>(p.at(k));
   }
 }
 // Bit k: a reset before step s0 + k.
-template <int N>
+template <int N, bool NARROW>
 __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
                                             int b, int s0) {
   unsigned m = 0;
   if (a.q.reset) {
     // all loads at once: none waits for another
     const SeqTensor t{(void*)a.q.reset, a.q.b, 1};
-    Walk<const uint8_t> w(t, r, b, 0, s0);
+    StepsAt<const uint8_t, NARROW> p(t, a.q, r, b, 0, s0);
     uint8_t x[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      x[k] = *w.p;
-      w.next();
+      x[k] = *p.here();
+      p.next(k);
     }
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -296,11 +278,26 @@ __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
 
 // Launches (defined beside their kernels).  Rows split along time: blocks of
 // kWaves (backward: kGradWaves) waves, one channel to a lane.  36001 steps of
-// 512 channels bf16, forward: 58 us; 82 with 4 waves, 57 with 16 (shorter rows
-// lose: 300 steps of 30 rows of 1023 channels 38 for 36); two channels to a
-// lane and half the steps 68.  Backward, 4099 steps of 8 rows: 77; 86 with 8
-// waves (a block's registers leave no room for a second beside it).
+// 512 channels bf16, forward: 54 us; 40% more with 4 waves, the same with 16
+// (shorter rows lose 6%: 300 steps of 30 rows of 1023 channels); two channels
+// to a lane and half the steps 17% more.  Backward, 4099 steps of 8 rows: 77;
+// 12% more with 8 waves (a block's registers leave no room for a second beside
+// it).
 constexpr int kWaves = 8, kGradWaves = 4;
+// Calls f(gated, narrow).
+template <class F>
+void with_scan_kind(const ScanArgs& a, F&& f) {
+  auto go = [&](auto gt) {
+    if (a.narrow)
+      f(gt, std::true_type{});
+    else
+      f(gt, std::false_type{});
+  };
+  if (a.o.p)
+    go(std::true_type{});
+  else
+    go(std::false_type{});
+}
 void launch_scan(const ScanArgs& a, int dtype, int out_dtype, int vec,
                  bool split, hipStream_t q);
 void launch_scan_backward(const ScanArgs& a, int dtype, int out_dtype,

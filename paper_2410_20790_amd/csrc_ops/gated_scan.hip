@@ -15,7 +15,7 @@ namespace {
 
 // Rows walked from their first step to their last, one thread to V channels of
 // a row, the loads of L steps in flight.
-template <typename T, typename O, int V, bool GATE>
+template <typename T, typename O, int V, bool GATE, bool NARROW>
 __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
   constexpr int L = kStride / V;
   const int64_t lane = (int64_t)blockIdx.x * kScanThreads + threadIdx.x;
@@ -28,11 +28,11 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
 #pragma unroll
   for (int e = 0; e < V; ++e) h[e] = a.h ? a.h[hc + e] : 0.f;
   for (int s = 0; s < r.len; s += L) {
-    const Whole w = whole_wave(a, r, s, L);
+    const bool whole = __all(s + L <= r.len);
     Pack<T, V> iv[L], jf[L], io[L];
-    load_steps<T, V, L>(a.f, w, a, r, b, ch, s, jf);
-    load_steps<T, V, L>(a.v, w, a, r, b, ch, s, iv);
-    if (GATE) load_steps<T, V, L>(a.o, w, a, r, b, ch, s, io);
+    load_steps<L, NARROW>(a.f, a, r, b, ch, s, whole, jf);
+    load_steps<L, NARROW>(a.v, a, r, b, ch, s, whole, iv);
+    if (GATE) load_steps<L, NARROW>(a.o, a, r, b, ch, s, whole, io);
     if (a.states && s % kStride == 0)
       store_pack<float, V>(a.states + (s / kStride) * plane + hc, h);
     auto step = [&](int k, O* y) {
@@ -49,12 +49,12 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
       }
       store_pack<O, V>(y, z);
     };
-    if (w.on && !a.q.reset) {
-      const WaveWalk<O> y(a.y, w.t, w.dir, b, ch);
+    if (whole && !a.q.reset) {
+      const StepsAt<O, NARROW> y(a.y, a.q, r, b, ch, s);
 #pragma unroll
       for (int k = 0; k < L; ++k) step(k, y.at(k));
     } else {
-      Walk<O> y(a.y, r, b, ch, s);
+      const StepsAt<O, NARROW> y(a.y, a.q, r, b, ch, s);
 #pragma unroll
       for (int k = 0; k < L; ++k) {
         if (s + k < r.len) {
@@ -62,8 +62,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
 #pragma unroll
             for (int e = 0; e < V; ++e) h[e] = 0.f;
           }
-          step(k, y.p);
-          y.next();
+          step(k, y.at(k));
         }
       }
     }
@@ -81,7 +80,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(ScanArgs a) {
   }
 }
 
-template <typename T, typename O, bool GATE, int W>
+template <typename T, typename O, bool GATE, bool NARROW, int W>
 __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   __shared__ TileShared<W> sh;
   const int ticket = next_ticket(a, sh);
@@ -93,18 +92,18 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   const int s0 = (tile * W + wave) * kSplit;
   float h = tile == 0 && a.h ? a.h[l.hc] : 0.f;
   const bool any = __any(s0 < r.len);
-  const Whole whole = whole_wave(a, r, s0, kSplit);
+  const bool whole = __all(s0 + kSplit <= r.len);
   float keep[kSplit], u[kSplit];
   Pack<T, 1> io[kSplit];
   unsigned cuts = 0;
   bool cutting = false;
   float A = 1.f, H = 0.f, TA, TH;
   if (any) {
-    cuts = cuts_of<kSplit>(a, r, l.b, s0);
+    cuts = cuts_of<kSplit, NARROW>(a, r, l.b, s0);
     Pack<T, 1> iv[kSplit], jf[kSplit];
-    load_steps<T, 1, kSplit>(a.f, whole, a, r, l.b, l.ch, s0, jf);
-    load_steps<T, 1, kSplit>(a.v, whole, a, r, l.b, l.ch, s0, iv);
-    if (GATE) load_steps<T, 1, kSplit>(a.o, whole, a, r, l.b, l.ch, s0, io);
+    load_steps<kSplit, NARROW>(a.f, a, r, l.b, l.ch, s0, whole, jf);
+    load_steps<kSplit, NARROW>(a.v, a, r, l.b, l.ch, s0, whole, iv);
+    if (GATE) load_steps<kSplit, NARROW>(a.o, a, r, l.b, l.ch, s0, whole, io);
 #pragma unroll
     for (int k = 0; k < kSplit; ++k) {
       float write;
@@ -112,7 +111,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
       u[k] = write * to_f(iv[k].e[0]);
     }
     // steps behind the row's end keep the state, to the bit
-    if (!whole.on) {
+    if (!whole) {
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         keep[k] = s0 + k < r.len ? keep[k] : 1.f;
@@ -148,22 +147,21 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
     auto gated = [&](int k) {
       return GATE ? h * sigmoid_once(to_f(io[k].e[0])) : h;
     };
-    if (whole.on && !cutting) {
-      const WaveWalk<O> ww(a.y, whole.t, whole.dir, l.b, l.ch);
+    if (whole && !cutting) {
+      const StepsAt<O, NARROW> y(a.y, a.q, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         h = __builtin_fmaf(keep[k], h, u[k]);
-        *ww.at(k) = from_f<O>(gated(k));
+        *y.at(k) = from_f<O>(gated(k));
       }
     } else {
-      Walk<O> wy(a.y, r, l.b, l.ch, s0);
+      const StepsAt<O, NARROW> y(a.y, a.q, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         if (s0 + k < r.len) {
           if (cuts >> k & 1) h = 0.f;
           h = __builtin_fmaf(keep[k], h, u[k]);
-          *wy.p = from_f<O>(gated(k));
-          wy.next();
+          *y.at(k) = from_f<O>(gated(k));
         }
       }
     }
@@ -184,13 +182,6 @@ __global__ __launch_bounds__(256) void k_scan_clear(uint4* w, int64_t n) {
 // -------------------------------------------------------------- host side
 
 template <class F>
-void with_gate(bool gate, F&& f) {
-  if (gate)
-    f(std::true_type{});
-  else
-    f(std::false_type{});
-}
-template <class F>
 void with_lane_vec(int v, F&& f) {
   if (v == 4)
     f(Int<4>{});
@@ -205,11 +196,13 @@ void with_lane_vec(int v, F&& f) {
 // by one: the same bits) of which there are too few to fill the device, a wave
 // for each 64 channels.  What fills it, measured on both sides (us, split and
 // walked, bf16, rows of 512 channels unless said):
-//   forward   1000 steps, 150 rows 177 and 246, 300 rows 340 and 296;
-//             100 steps, 300 rows of 256 channels 21 and 26
-//   backward  1000 steps, 150 rows 281 and 379, 300 rows 547 and 690;
-//             300 steps, 600 rows 348 and 349; 100 steps of 256 channels,
-//             300 rows 46 and 36; 100 steps of 8 rows 12 and 23
+//   forward   1000 steps, 150 rows 163 and 266, 300 rows 314 and 317;
+//             300 steps, 200 rows 76 and 71; 100 steps, 300 rows of 256
+//             channels 19 and 26
+//   backward  1000 steps, 150 rows 272 and 377, 300 rows 534 and 501;
+//             300 steps, 400 rows 227 and 240, 600 rows 337 and 286;
+//             100 steps, 300 rows of 256 channels 46 and 38, 200 rows 37 and
+//             32; 60 steps of 8 rows 8 and 17
 constexpr int kSerialSteps = 32, kShortSteps = 128;
 constexpr int64_t kFillWaves = 2048;    // eight to a CU
 int64_t split_waves(const st_seq_desc& d, bool backward) {
@@ -285,14 +278,14 @@ void launch_scan(const ScanArgs& a, int dtype, int out_dtype, int vec,
   with_types(dtype, out_dtype, [&](auto ti, auto to) {
     using T = typename decltype(ti)::type;
     using O = typename decltype(to)::type;
-    with_gate(a.o.p != nullptr, [&](auto gt) {
-      constexpr bool G = decltype(gt)::value;
+    with_scan_kind(a, [&](auto gt, auto nt) {
+      constexpr bool G = decltype(gt)::value, N = decltype(nt)::value;
       if (split)
-        k_scan_tiles<T, O, G, kWaves>
+        k_scan_tiles<T, O, G, N, kWaves>
             <<<(unsigned)(a.cols * a.tiles), 64 * kWaves, 0, q>>>(a);
       else
         with_lane_vec(vec, [&](auto vt) {
-          k_scan<T, O, decltype(vt)::value, G>
+          k_scan<T, O, decltype(vt)::value, G, N>
               <<<(unsigned)ceil_div(a.lanes, kScanThreads), kScanThreads, 0,
                  q>>>(a);
         });
@@ -367,8 +360,10 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.o = tensor_of(o);
     a.y = tensor_of(y);
     a.stream = streamed(*d, (o ? 3 : 2) * es);
-    a.narrow = narrow(*d, v, es) && narrow(*d, f, es) && narrow(*d, o, es) &&
-               narrow(*d, y, eo);
+    const st_seq_ref rs{nullptr, d->b, 1};
+    a.narrow = narrow(*d, v, es) && narrow(*d, f, es) &&
+               narrow(*d, o, es) && narrow(*d, y, eo) &&
+               narrow(*d, &rs, 1);
     a.h = h;
     a.h_out = h_out;
     a.states = states;
@@ -446,7 +441,8 @@ extern "C" st_status st_gated_scan_backward(
     a.df = tensor_of(df);
     a.d_o = tensor_of(d_o);
     a.stream = streamed(*d, (o ? 3 : 2) * es + eo);
-    a.narrow = narrow(*d, dy, eo);
+    const st_seq_ref rs{nullptr, d->b, 1};
+    a.narrow = narrow(*d, dy, eo) && narrow(*d, &rs, 1);
     for (const st_seq_ref* r : {v, f, o, dv, df, d_o})
       a.narrow = a.narrow && narrow(*d, r, es);
     a.h = dh_out;

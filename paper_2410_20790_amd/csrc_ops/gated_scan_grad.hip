@@ -12,71 +12,67 @@ namespace st {
 namespace ops {
 namespace {
 
-// (A channel to a lane: four arrays of 16 steps in registers leave no room for
-// a second.)
-//
 // kSplit steps of a lane: their states come again from the one kept before
-// them, forward; the gradients go back through them.  All is read once.
-template <typename T, typename O, bool GATE>
+// them, forward; the gradients go back through them.  All is read once.  (A
+// channel to a lane: four arrays of 16 steps in registers leave no room for a
+// second.)
+//
+// TWO: whole waves have a path of their own, without a test at every step.
+// Rows split along time gain by it (36 us for 41, 100 steps of 300 rows of 256
+// channels); rows that are walked, with all else in the same loop, lose a wave
+// of each SIMD to its registers (9 steps of 2048 rows of 1024 channels f32 114
+// us for 135).
+template <typename T, typename O, bool GATE, bool NARROW, bool TWO>
 struct GradSteps {
   float keep[kSplit], write[kSplit];
   float g[kSplit];     // dy sigmoid(o)
   float q[kSplit];     // h_{s-1} - v
-  Whole whole;
+  bool whole;          // all lanes of the wave have all steps
   unsigned cuts;
 
   // Loads, states, and do.
   __device__ __forceinline__ void forward(const ScanArgs& a, const Row& r,
                                           const LaneAt& l, int s0) {
-    whole = whole_wave(a, r, s0, kSplit);
+    whole = __all(s0 + kSplit <= r.len);
     Pack<T, 1> iv[kSplit], jf[kSplit], io[kSplit];
     Pack<O, 1> id[kSplit];
-    load_steps<T, 1, kSplit>(a.f, whole, a, r, l.b, l.ch, s0, jf);
-    load_steps<T, 1, kSplit>(a.v, whole, a, r, l.b, l.ch, s0, iv);
-    if (GATE) load_steps<T, 1, kSplit>(a.o, whole, a, r, l.b, l.ch, s0, io);
-    load_steps<O, 1, kSplit>(a.y, whole, a, r, l.b, l.ch, s0, id);
+    load_steps<kSplit, NARROW>(a.f, a, r, l.b, l.ch, s0, whole, jf);
+    load_steps<kSplit, NARROW>(a.v, a, r, l.b, l.ch, s0, whole, iv);
+    if (GATE) load_steps<kSplit, NARROW>(a.o, a, r, l.b, l.ch, s0, whole, io);
+    load_steps<kSplit, NARROW>(a.y, a, r, l.b, l.ch, s0, whole, id);
     float h = 0.f;
     if (s0 < r.len)
       h = a.states[(s0 / kStride) * ((int64_t)a.q.b * a.q.c) + l.hc];
-    cuts = cuts_of<kSplit>(a, r, l.b, s0);
-    auto step = [&](int k) {
-      const bool cut = cuts >> k & 1;
+    cuts = cuts_of<kSplit, NARROW>(a, r, l.b, s0);
+    // a step's values; its do, to out
+    auto step = [&](int k, T* out, bool put) {
       const float v = to_f(iv[k].e[0]);
-      g[k] = to_f(id[k].e[0]);
       sigmoids(to_f(jf[k].e[0]), keep[k], write[k]);
-      h = cut ? 0.f : h;
+      h = cuts >> k & 1 ? 0.f : h;
       q[k] = h - v;
       h = __builtin_fmaf(keep[k], h, write[k] * v);
-      if constexpr (GATE) {
+      g[k] = to_f(id[k].e[0]);
+      if (GATE) {
         float p, n;
         sigmoids_once(to_f(io[k].e[0]), p, n);
         g[k] *= p;
-        return g[k] * h * n;
-      } else {
-        return 0.f;
+        const float go = g[k] * h * n;
+        if (put) *out = from_f<T>(go);
       }
     };
-    if (whole.on && __all(l.on)) {
-      const WaveWalk<T> w(GATE ? a.d_o : a.dv, whole.t, whole.dir, l.b, l.ch);
+    const SeqTensor& to = GATE ? a.d_o : a.dv;
+    if (TWO && whole && __all(l.on)) {
+      const StepsAt<T, NARROW> out(to, a.q, r, l.b, l.ch, s0);
 #pragma unroll
-      for (int k = 0; k < kSplit; ++k) {
-        const float go = step(k);
-        if (GATE) *w.at(k) = from_f<T>(go);
-      }
+      for (int k = 0; k < kSplit; ++k) step(k, out.at(k), true);
     } else {
-      Walk<T> w(GATE ? a.d_o : a.dv, r, l.b, l.ch, s0);
+      const StepsAt<T, NARROW> out(to, a.q, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         // behind the row's end: what comes back passes as it is
         keep[k] = 1.f;
         write[k] = g[k] = q[k] = 0.f;
-        if (s0 + k < r.len) {
-          const float go = step(k);
-          if (GATE && l.on) {
-            *w.p = from_f<T>(go);
-            w.next();
-          }
-        }
+        if (s0 + k < r.len) step(k, out.at(k), l.on);
       }
     }
   }
@@ -97,30 +93,23 @@ struct GradSteps {
   __device__ __forceinline__ void back(const ScanArgs& a, const Row& r,
                                        const LaneAt& l, int s0, float& dh) {
     auto step = [&](int k, T* dv, T* df) {
-      const bool cut = cuts >> k & 1;
       dh += g[k];
       const float gv = dh * write[k];
       *dv = from_f<T>(gv);
       *df = from_f<T>(gv * q[k] * keep[k]);
-      dh = cut ? 0.f : dh * keep[k];
+      dh = cuts >> k & 1 ? 0.f : dh * keep[k];
     };
-    if (whole.on) {
-      const WaveWalk<T> wv(a.dv, whole.t, whole.dir, l.b, l.ch),
-          wf(a.df, whole.t, whole.dir, l.b, l.ch);
+    if (whole) {
+      const StepsAt<T, NARROW> dv(a.dv, a.q, r, l.b, l.ch, s0),
+          df(a.df, a.q, r, l.b, l.ch, s0);
 #pragma unroll
-      for (int k = kSplit - 1; k >= 0; --k) step(k, wv.at(k), wf.at(k));
+      for (int k = kSplit - 1; k >= 0; --k) step(k, dv.at(k), df.at(k));
     } else {
-      // back from the last of the steps that the row has
-      Walk<T> wv(a.dv, r, l.b, l.ch, s0 + kSplit - 1),
-          wf(a.df, r, l.b, l.ch, s0 + kSplit - 1);
+      const StepsAt<T, NARROW> dv(a.dv, a.q, r, l.b, l.ch, s0),
+          df(a.df, a.q, r, l.b, l.ch, s0);
 #pragma unroll
-      for (int k = kSplit - 1; k >= 0; --k) {
-        if (s0 + k < r.len) {
-          step(k, wv.p, wf.p);
-          wv.p -= wv.step;
-          wf.p -= wf.step;
-        }
-      }
+      for (int k = kSplit - 1; k >= 0; --k)
+        if (s0 + k < r.len) step(k, dv.at(k), df.at(k));
     }
   }
 };
@@ -140,7 +129,7 @@ __device__ __forceinline__ void zero_behind(const ScanArgs& a, const Row& r,
 }
 
 // Rows walked from their last step to their first, kSplit steps at a time.
-template <typename T, typename O, bool GATE>
+template <typename T, typename O, bool GATE, bool NARROW>
 __global__ __launch_bounds__(kScanThreads) void k_scan_grad(ScanArgs a) {
   const int64_t lane = (int64_t)blockIdx.x * kScanThreads + threadIdx.x;
   if (lane >= a.lanes) return;
@@ -155,7 +144,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_grad(ScanArgs a) {
   // (every lane from the last step of all rows: their times stay the same)
   for (int s0 = (a.q.t - 1) / kSplit * kSplit; s0 >= 0; s0 -= kSplit) {
     if (s0 < r.len) {
-      GradSteps<T, O, GATE> steps;
+      GradSteps<T, O, GATE, NARROW, false> steps;
       steps.forward(a, r, l, s0);
       steps.back(a, r, l, s0, dh);
     }
@@ -164,7 +153,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_grad(ScanArgs a) {
 }
 
 // Rows split along time: tiles and waves run from the row's last step.
-template <typename T, typename O, bool GATE, int W>
+template <typename T, typename O, bool GATE, bool NARROW, int W>
 __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
   __shared__ TileShared<W> sh;
   const int ticket = next_ticket(a, sh);
@@ -175,7 +164,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_tiles(ScanArgs a) {
   const int s0 = ((a.tiles - 1 - k_th) * W + W - 1 - wave) * kSplit;
   float dh = k_th == 0 && a.h ? a.h[l.hc] : 0.f;
   const bool any = __any(s0 < r.len);
-  GradSteps<T, O, GATE> steps;
+  GradSteps<T, O, GATE, NARROW, true> steps;
   float A = 1.f, D = 0.f, TA, TD;
   if (any) {
     steps.forward(a, r, l, s0);
@@ -200,20 +189,16 @@ void launch_scan_backward(const ScanArgs& a, int dtype, int out_dtype,
   with_types(dtype, out_dtype, [&](auto ti, auto to) {
     using T = typename decltype(ti)::type;
     using O = typename decltype(to)::type;
-    auto go = [&](auto gt) {
-      constexpr bool G = decltype(gt)::value;
+    with_scan_kind(a, [&](auto gt, auto nt) {
+      constexpr bool G = decltype(gt)::value, N = decltype(nt)::value;
       if (split)
-        k_scan_grad_tiles<T, O, G, kGradWaves>
+        k_scan_grad_tiles<T, O, G, N, kGradWaves>
             <<<(unsigned)(a.cols * a.tiles), 64 * kGradWaves, 0, q>>>(a);
       else
-        k_scan_grad<T, O, G>
+        k_scan_grad<T, O, G, N>
             <<<(unsigned)ceil_div(a.lanes, kScanThreads), kScanThreads, 0,
                q>>>(a);
-    };
-    if (a.o.p)
-      go(std::true_type{});
-    else
-      go(std::false_type{});
+    });
   });
 }
 

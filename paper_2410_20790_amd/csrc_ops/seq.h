@@ -70,30 +70,62 @@ struct Walk {
   }
 };
 
-// The same for a whole wave whose lanes all have the steps at one time: a
-// scalar address that moves by steps and one 32-bit offset per lane, so that
-// the addresses of many loads in flight take no vector registers.
-template <typename T>
-struct WaveWalk {
+// Running steps s0, s0 + 1, ... of a row: a scalar address that moves by steps
+// and one offset per lane (NARROW: of 32 bits), so that the addresses of many
+// loads in flight take no vector registers.  Times differ from lane to lane
+// only where rows of their own lengths run backwards; there the offset holds
+// the row's time.  Offsets never fall below zero: rows that run backwards begin
+// kAheadSteps steps into theirs.
+constexpr int kAheadSteps = ST_SCAN_STRIDE;   // steps of one of these, at most
+template <typename T, bool NARROW>
+struct StepsAt {
+  typedef std::conditional_t<NARROW, uint32_t, int64_t> Off;
   char* p;
   int64_t step;
-  uint32_t off;
-  __device__ __forceinline__ WaveWalk(const SeqTensor& x, int64_t t, int dir,
-                                      int b, int ch) {
-    p = (char*)x.p + t * x.st * (int64_t)sizeof(T);
-    step = dir * x.st * (int64_t)sizeof(T);
-    off = (uint32_t)(((int64_t)b * x.sb + ch) * (int64_t)sizeof(T));
+  Off off;
+  int left;      // steps that the row has after s0
+  __device__ __forceinline__ StepsAt(const SeqTensor& x, const SeqAxes& q,
+                                     const Row& r, int b, int ch, int s0) {
+    const int64_t es = sizeof(T);
+    left = max(r.len - 1 - s0, 0);
+    int64_t at = (int64_t)b * x.sb + ch, t = s0;
+    if (q.reverse) {
+      t = q.t - 1 - s0;
+      if (q.lengths) {
+        t = 0;
+        at += left * x.st;
+      } else {
+        t -= kAheadSteps;
+        at += kAheadSteps * x.st;
+      }
+    }
+    p = (char*)x.p + t * x.st * es;
+    step = q.reverse ? -x.st * es : x.st * es;
+    off = (Off)(at * es);
+    // (formed anew wherever it is used: across blocks the compiler would keep
+    // it added to the address, two registers for every load in flight)
+    if constexpr (NARROW) asm volatile("" : "+v"(off));
   }
+  // Step s0 + k, which the row must have.
   __device__ __forceinline__ T* at(int k) const {
     return (T*)(p + k * step + off);
+  }
+  // The same one by one: on to the next step, or to where the row ends.
+  __device__ __forceinline__ T* here() const { return (T*)(p + off); }
+  __device__ __forceinline__ void next(int k) {     // from step s0 + k
+    off += k < left ? (Off)step : 0;
   }
 };
 
 // -------------------------------------------------------------- host side
 
-// Whether a lane's offset within one time of the tensor fits 32 bits.
+// Whether a lane's offset fits 32 bits: within kAheadSteps times of the tensor,
+// or (rows of their own lengths that run backwards) within all of it.
 inline bool narrow(const st_seq_desc& d, const st_seq_ref* r, int es) {
-  return !r || ((int64_t)(d.b - 1) * r->stride_b + d.c) * es < (int64_t)1 << 31;
+  if (!r) return true;
+  const int64_t times = d.lengths && d.reverse ? d.t : kAheadSteps;
+  return ((d.b - 1) * r->stride_b + times * r->stride_t + d.c) * es <
+         (int64_t)1 << 31;
 }
 inline SeqAxes axes_of(const st_seq_desc& d) {
   return SeqAxes{d.t, d.b, d.c, d.reverse != 0, d.lengths, d.reset};

@@ -616,3 +616,34 @@ def test_tensor_refusals():
                 out=(x.clone(), x.clone())))):
         with pytest.raises(err):
             fn()
+
+
+@pytest.mark.parametrize("t", [20, 40])
+@pytest.mark.parametrize("kind", ["", "b", "l", "lb", "lrb"])
+@pytest.mark.parametrize("step", [2 ** 26 - 2 ** 10, 2 ** 26 + 2 ** 10])
+def test_scan_steps_far_apart(t, kind, step):
+    """Steps so far apart that 16 of them reach over 2^31 bytes, or just not:
+    the same bits as from tensors without gaps."""
+    say(f"[gpu] gated scan, steps {step} elements apart, {t} {kind!r}")
+    b, c = 5, 8
+    ln, rs, rev = axes(kind, t, b)
+    kw = dict(lengths=dev(ln), reset=dev(rs), reverse=rev)
+    def apart(n):       # n tensors side by side
+        room = torch.empty(t * step, dtype=BF16, device="cuda")
+        return tuple(room.as_strided((t, b, c), (step, n * c, 1), i * c)
+                     for i in range(n))
+    wide = apart(4)
+    tight = [rnd(160 + i, t, b, c, dtype=BF16) for i in range(4)]
+    for x, y in zip(wide, tight):
+        x.copy_(y)
+    h, dh = rnd(165, b, c), rnd(166, b, c)
+    y, ho, st = ops.gated_scan(*tight[:3], h=h, save=True, **kw)
+    yw, hw, sw = ops.gated_scan(*wide[:3], h=h, save=True, out=apart(1)[0],
+                                **kw)
+    assert torch.equal(y, yw) and torch.equal(ho, hw)
+    grads = ops.gated_scan_backward(tight[3], *tight[:3], states=st, dh=dh,
+                                    **kw)
+    got = ops.gated_scan_backward(wide[3], *wide[:3], states=sw, dh=dh,
+                                  out=apart(3), **kw)
+    for p, q in zip(grads, got):
+        assert torch.equal(p, q)
