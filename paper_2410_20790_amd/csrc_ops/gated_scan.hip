@@ -361,9 +361,10 @@ extern "C" st_status st_gated_scan(const st_seq_desc* d, const st_seq_ref* v,
     a.y = tensor_of(y);
     a.stream = streamed(*d, (o ? 3 : 2) * es);
     const st_seq_ref rs{nullptr, d->b, 1};
-    a.narrow = narrow(*d, v, es) && narrow(*d, f, es) &&
-               narrow(*d, o, es) && narrow(*d, y, eo) &&
-               narrow(*d, &rs, 1);
+    const int64_t reach = steps_reach(*d);
+    a.narrow = narrow(*d, y, eo, reach) && narrow(*d, &rs, 1, reach);
+    for (const st_seq_ref* r : {v, f, o})
+      a.narrow = a.narrow && narrow(*d, r, es, reach);
     a.h = h;
     a.h_out = h_out;
     a.states = states;
@@ -442,9 +443,10 @@ extern "C" st_status st_gated_scan_backward(
     a.d_o = tensor_of(d_o);
     a.stream = streamed(*d, (o ? 3 : 2) * es + eo);
     const st_seq_ref rs{nullptr, d->b, 1};
-    a.narrow = narrow(*d, dy, eo) && narrow(*d, &rs, 1);
+    const int64_t reach = steps_reach(*d);
+    a.narrow = narrow(*d, dy, eo, reach) && narrow(*d, &rs, 1, reach);
     for (const st_seq_ref* r : {v, f, o, dv, df, d_o})
-      a.narrow = a.narrow && narrow(*d, r, es);
+      a.narrow = a.narrow && narrow(*d, r, es, reach);
     a.h = dh_out;
     a.h_out = dh;
     a.states = const_cast<float*>(states);

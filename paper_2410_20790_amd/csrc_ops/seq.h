@@ -45,28 +45,34 @@ __device__ __forceinline__ bool reset_at(const SeqAxes& q, const Row& r,
   return q.reset && q.reset[time_of(r, s) * q.b + b] != 0;
 }
 
-// A row's elements in running order, from step s0 on: next() goes to the
-// next step, or stays where the row ends (an address that may be read, time 0
-// of a row of no steps).  One addition per step; the products that a time and
-// its stride make up are formed once.
-template <typename T>
+// A row's elements in running order, from step s0 on: next() goes to the next
+// step, or stays where the row ends (an address that may be read, time 0 of a
+// row of no steps).  One addition per step; the products that a time and its
+// stride make up are formed once.  NARROW: offsets of 32 bits into the tensor.
+template <typename T, bool NARROW>
 struct Walk {
-  T* p;
-  int64_t step;
+  typedef std::conditional_t<NARROW, uint32_t, int64_t> Off;
+  char* p;
+  Off off, step;
   int left;    // steps that may follow
   __device__ __forceinline__ Walk(const SeqTensor& x, const Row& r, int b,
                                   int ch, int s0) {
     const int last = max(r.len - 1, 0), s = min(s0, last);
-    const int64_t t = r.len > 0 ? time_of(r, s) : 0;
-    p = (T*)x.p + t * x.st + (int64_t)b * x.sb + ch;
-    step = r.dir * x.st;
+    const int64_t t = r.len > 0 ? time_of(r, s) : 0, es = sizeof(T);
+    p = (char*)x.p;
+    off = (Off)((t * x.st + (int64_t)b * x.sb + ch) * es);
+    step = (Off)(r.dir * x.st * es);
     left = last - s;
   }
+  __device__ __forceinline__ T* here() const {
+    Off o = off;
+    // (added to the address here, as the instruction does by itself)
+    if constexpr (NARROW) asm volatile("" : "+v"(o));
+    return (T*)(p + o);
+  }
   __device__ __forceinline__ void next() {
-    if (left > 0) {
-      p += step;
-      --left;
-    }
+    off += left > 0 ? step : 0;
+    --left;
   }
 };
 
@@ -119,13 +125,16 @@ struct StepsAt {
 
 // -------------------------------------------------------------- host side
 
-// Whether a lane's offset fits 32 bits: within kAheadSteps times of the tensor,
-// or (rows of their own lengths that run backwards) within all of it.
-inline bool narrow(const st_seq_desc& d, const st_seq_ref* r, int es) {
-  if (!r) return true;
-  const int64_t times = d.lengths && d.reverse ? d.t : kAheadSteps;
-  return ((d.b - 1) * r->stride_b + times * r->stride_t + d.c) * es <
-         (int64_t)1 << 31;
+// Whether offsets into `times` times of a tensor fit 32 bits.
+inline bool narrow(const st_seq_desc& d, const st_seq_ref* r, int es,
+                   int64_t times) {
+  return !r || ((d.b - 1) * r->stride_b + times * r->stride_t + d.c) * es <
+                   (int64_t)1 << 31;
+}
+// The times that StepsAt reaches over: all of them where rows of their own
+// lengths run backwards.
+inline int64_t steps_reach(const st_seq_desc& d) {
+  return d.lengths && d.reverse ? d.t : kAheadSteps;
 }
 inline SeqAxes axes_of(const st_seq_desc& d) {
   return SeqAxes{d.t, d.b, d.c, d.reverse != 0, d.lengths, d.reset};

@@ -27,6 +27,7 @@ struct ConvTimeArgs {
   int colblocks;
   int tile, tiles;       // steps per unit, units per row
   int gridy;
+  int narrow;            // 32-bit offsets (see Walk)
 };
 
 __device__ __forceinline__ float act_any(int act, float z) {

@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kAhead = 4;   // steps whose loads a thread has in flight
 
-template <typename T, typename O, int V, int K>
+template <typename T, typename O, int V, int K, bool NARROW>
 __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
   const int col = threadIdx.x % a.cols, row = threadIdx.x / a.cols;
   const int cb = blockIdx.x % a.colblocks;
@@ -40,13 +40,13 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
     const int end = min(s1, r.len);
     float win[K > 1 ? K - 1 : 1][V];
     if (s0 < end) load_window<T, V, K>(a, r, b, ch, s0, win);
-    Walk<const T> wx(a.x, r, b, ch, s0);
-    Walk<O> wy(a.y, r, b, ch, s0);
+    Walk<const T, NARROW> wx(a.x, r, b, ch, s0);
+    Walk<O, NARROW> wy(a.y, r, b, ch, s0);
     for (int s = s0; s < end; s += kAhead) {
       Pack<T, V> in[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        in[k] = load_pack<T, V>(wx.p);
+        in[k] = load_pack<T, V>(wx.here());
         wx.next();
       }
 #pragma unroll
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
             z[e] = __builtin_fmaf(w[K - 1][e], f[e], z[e]);
             z[e] = act_any(a.act, z[e]);
           }
-          store_pack<O, V>(wy.p, z);
+          store_pack<O, V>(wy.here(), z);
           wy.next();
 #pragma unroll
           for (int e = 0; e < V; ++e) {
@@ -115,10 +115,14 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv(ConvTimeArgs a) {
 
 // -------------------------------------------------------------- host side
 
-constexpr int64_t kFillThreads = 256 * 1024;  // four waves to a SIMD
+// Threads that a call is cut for: four waves to a SIMD; the backward pass, whose
+// tiles have a longer halo, three (601 steps of 48 rows of 512 channels f16 34
+// us, 36 with four and 35 with two; 1000 steps of 64 rows of 512 channels bf16
+// 45, 46 and 53).
+constexpr int64_t kFillThreads = 256 * 1024, kGradThreads = 192 * 1024;
 // Channels to a thread of the backward pass, whose registers hold three
-// windows: two measured 46 us where four take 53 and one 57 (gradients of
-// 20000 steps of 1024 channels bf16).
+// windows: two, 1000 steps of 64 rows of 512 channels bf16 45 us for 50 with
+// one (300 steps of 20 rows of 1024 channels 25 for 23); four take 15% more.
 constexpr int kGradVec = 2;
 constexpr int kTargetBlocks = 1024;
 
@@ -137,7 +141,7 @@ ConvCut cut_of(const st_seq_desc& d, int taps, bool backward, int v) {
   const int64_t lanes = (int64_t)d.b * c.cv;
   const int64_t least = std::max(8, 4 * (taps - 1));
   const int64_t want = ceil_div((int64_t)d.t * std::max<int64_t>(lanes, 1),
-                                kFillThreads);
+                                backward ? kGradThreads : kFillThreads);
   c.tile = (int)std::max(least, std::min<int64_t>(want, 1 << 20));
   c.tiles = (int)std::max<int64_t>(1, ceil_div(d.t, c.tile));
   const int64_t need = ceil_div((int64_t)c.tiles * d.b, c.rows);
@@ -177,8 +181,13 @@ void launch_time_conv(const ConvTimeArgs& a, int dtype, int out_dtype,
     using O = typename decltype(to)::type;
     with_conv_vec(vec, [&](auto vt) {
       with_taps(taps, [&](auto kt) {
-        k_time_conv<T, O, decltype(vt)::value, decltype(kt)::value>
-            <<<grid, kConvThreads, 0, stream>>>(a);
+        constexpr int V = decltype(vt)::value, K = decltype(kt)::value;
+        if (a.narrow)
+          k_time_conv<T, O, V, K, true>
+              <<<grid, kConvThreads, 0, stream>>>(a);
+        else
+          k_time_conv<T, O, V, K, false>
+              <<<grid, kConvThreads, 0, stream>>>(a);
       });
     });
   });
@@ -252,6 +261,7 @@ extern "C" st_status st_time_conv(const st_seq_desc* d, int32_t taps,
     a.cv = c.cv; a.cols = c.cols; a.rows = c.rows;
     a.colblocks = c.colblocks;
     a.tile = c.tile; a.tiles = c.tiles; a.gridy = c.gridy;
+    a.narrow = narrow(*d, x, es, d->t) && narrow(*d, y, eo, d->t);
     launch_time_conv(a, d->dtype, d->out_dtype, taps, v, (hipStream_t)stream);
     return launch_status("time convolution");
   });
@@ -321,6 +331,8 @@ extern "C" st_status st_time_conv_backward(
     a.colblocks = c.colblocks;
     a.tile = c.tile; a.tiles = c.tiles;
     a.gridy = d->b == 0 ? 0 : c.gridy;
+    a.narrow = narrow(*d, x, es, d->t) && narrow(*d, dy, eo, d->t) &&
+               narrow(*d, dx, es, d->t);
     launch_time_conv_backward(a, d->dtype, d->out_dtype, taps, v,
                               (hipStream_t)stream);
     return launch_status("time convolution backward");

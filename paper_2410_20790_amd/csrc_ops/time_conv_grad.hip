@@ -17,8 +17,16 @@ namespace ops {
 namespace {
 
 constexpr int kAhead = 4;
+// PLAIN: no resets, and steps inside a tile have a path of their own that tests
+// for nothing.  It takes a quarter more registers: for tiles (or rows) of some
+// length, and as many channels and taps as still leave four waves to a SIMD.
+// us, with and without: 601 steps of 48 rows of 512 channels f16, 4 taps 34 and
+// 38; 300 steps of 30 rows of 1023 channels, 5 taps 28 and 33; 9 steps of 2048
+// rows of 512 channels f32 45 and 39; 64 steps of 512 rows of 256 channels, 8
+// taps 40 and 37.
+constexpr int kPlainSteps = 16, kPlainTaps = 10;   // taps times channels
 
-template <typename T, typename O, int V, int K>
+template <typename T, typename O, int V, int K, bool NARROW, bool PLAIN>
 __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
     ConvTimeArgs a) {
   const int col = threadIdx.x % a.cols, row = threadIdx.x / a.cols;
@@ -55,7 +63,7 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[i][e] = 0.f;
     // the finished dx of position p (in rising order)
-    Walk<T> dx(a.dx, r, b, ch, s0);
+    Walk<T, NARROW> dx(a.dx, r, b, ch, s0);
     auto put = [&](int p, float* v) {
       if (p < first || p >= own) return;
       const int i = p - (r.len - (K - 1));      // its place in window_out
@@ -68,7 +76,7 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
         for (int e = 0; e < V; ++e) v[e] += g[e];
       }
       if (p >= 0) {
-        if (a.dx.p) store_pack<T, V>(dx.p, v);
+        if (a.dx.p) store_pack<T, V>(dx.here(), v);
         dx.next();
       } else if (a.dwindow) {
         store_pack<T, V>((T*)a.dwindow +
@@ -80,16 +88,16 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
       int open = K;    // taps back that no reset hides
       if (s0 < own) load_window<T, V, K>(a, r, b, ch, s0, win);
       int s = s0;
-      Walk<const T> x(a.x, r, b, ch, s0);
-      Walk<const O> dy(a.dy, r, b, ch, s0);
+      Walk<const T, NARROW> x(a.x, r, b, ch, s0);
+      Walk<const O, NARROW> dy(a.dy, r, b, ch, s0);
       // the next steps' loads are in flight while these are worked on
       Pack<T, V> xn[kAhead];
       Pack<O, V> dn[kAhead];
       auto fetch = [&] {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          xn[k] = load_pack<T, V>(x.p);
-          dn[k] = load_pack<O, V>(dy.p);
+          xn[k] = load_pack<T, V>(x.here());
+          dn[k] = load_pack<O, V>(dy.here());
           x.next();
           dy.next();
         }
@@ -104,52 +112,63 @@ __global__ __launch_bounds__(kConvThreads) void k_time_conv_grad(
           di[k] = dn[k];
         }
         if (s + kAhead < end) fetch();
+        auto step = [&](int k, auto pt) __attribute__((always_inline)) {
+          constexpr bool P = decltype(pt)::value;
+          float f[V], d[V], out[V];
+          unpack<T, V>(xi[k], f);
+          unpack<O, V>(di[k], d);
+          if (!PLAIN && reset_at(a.q, r, b, s + k)) {
+            open = 0;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          if (s + k < end) {
-            float f[V], d[V], out[V];
-            unpack<T, V>(xi[k], f);
-            unpack<O, V>(di[k], d);
-            if (reset_at(a.q, r, b, s + k)) {
-              open = 0;
+            for (int j = 0; j < K - 1; ++j)
 #pragma unroll
-              for (int j = 0; j < K - 1; ++j)
+              for (int e = 0; e < V; ++e) win[j][e] = 0.f;
+          }
+          const bool mine = P || s + k < s1;
 #pragma unroll
-                for (int e = 0; e < V; ++e) win[j][e] = 0.f;
-            }
-            const bool mine = s + k < s1;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              if (a.act != ST_ACT_NONE) {
-                float z = bias[e];
-#pragma unroll
-                for (int j = 0; j < K - 1; ++j)
-                  z = __builtin_fmaf(w[j][e], win[j][e], z);
-                z = __builtin_fmaf(w[K - 1][e], f[e], z);
-                d[e] *= act_grad_any(a.act, z);
-              }
-              const float m = mine ? d[e] : 0.f;
-              db[e] += m;
+          for (int e = 0; e < V; ++e) {
+            if (a.act != ST_ACT_NONE) {
+              float z = bias[e];
 #pragma unroll
               for (int j = 0; j < K - 1; ++j)
-                dw[j][e] = __builtin_fmaf(m, win[j][e], dw[j][e]);
-              dw[K - 1][e] = __builtin_fmaf(m, f[e], dw[K - 1][e]);
-              // acc[j] is position s + k - (K - 1) + j, tap j
-#pragma unroll
-              for (int j = 0; j < K; ++j)
-                if (K - 1 - j <= open)
-                  acc[j][e] = __builtin_fmaf(w[j][e], d[e], acc[j][e]);
-              out[e] = acc[0][e];
-#pragma unroll
-              for (int j = 0; j + 1 < K; ++j) acc[j][e] = acc[j + 1][e];
-              acc[K - 1][e] = 0.f;
-#pragma unroll
-              for (int j = 0; j + 1 < K - 1; ++j) win[j][e] = win[j + 1][e];
-              if (K > 1) win[K > 1 ? K - 2 : 0][e] = f[e];
+                z = __builtin_fmaf(w[j][e], win[j][e], z);
+              z = __builtin_fmaf(w[K - 1][e], f[e], z);
+              d[e] *= act_grad_any(a.act, z);
             }
+            const float m = mine ? d[e] : 0.f;
+            db[e] += m;
+#pragma unroll
+            for (int j = 0; j < K - 1; ++j)
+              dw[j][e] = __builtin_fmaf(m, win[j][e], dw[j][e]);
+            dw[K - 1][e] = __builtin_fmaf(m, f[e], dw[K - 1][e]);
+            // acc[j] is position s + k - (K - 1) + j, tap j
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+              if (PLAIN || K - 1 - j <= open)
+                acc[j][e] = __builtin_fmaf(w[j][e], d[e], acc[j][e]);
+            out[e] = acc[0][e];
+#pragma unroll
+            for (int j = 0; j + 1 < K; ++j) acc[j][e] = acc[j + 1][e];
+            acc[K - 1][e] = 0.f;
+#pragma unroll
+            for (int j = 0; j + 1 < K - 1; ++j) win[j][e] = win[j + 1][e];
+            if (K > 1) win[K > 1 ? K - 2 : 0][e] = f[e];
+          }
+          if constexpr (P) {
+            if (a.dx.p) store_pack<T, V>(dx.here(), out);
+            dx.next();
+          } else {
             open = min(open + 1, K);
             put(s + k - (K - 1), out);
           }
+        };
+        if (PLAIN && __all(s >= s0 + K - 1 && s + kAhead <= own)) {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) step(k, std::true_type{});
+        } else {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (s + k < end) step(k, std::false_type{});
         }
       }
       // positions that no further step reaches
@@ -229,9 +248,20 @@ void launch_time_conv_backward(const ConvTimeArgs& a, int dtype,
       using O = typename decltype(to)::type;
       with_conv_vec(vec, [&](auto vt) {
         with_taps(taps, [&](auto kt) {
-          if constexpr (decltype(vt)::value <= 2)
-            k_time_conv_grad<T, O, decltype(vt)::value, decltype(kt)::value>
-                <<<grid, kConvThreads, 0, stream>>>(a);
+          constexpr int V = decltype(vt)::value, K = decltype(kt)::value;
+          if constexpr (V <= 2) {
+            constexpr bool fits = V * K <= kPlainTaps;
+            if (!a.narrow)
+              k_time_conv_grad<T, O, V, K, false, false>
+                  <<<grid, kConvThreads, 0, stream>>>(a);
+            else if (fits && !a.q.reset &&
+                     std::min(a.tile, a.q.t) >= kPlainSteps)
+              k_time_conv_grad<T, O, V, K, true, fits>
+                  <<<grid, kConvThreads, 0, stream>>>(a);
+            else
+              k_time_conv_grad<T, O, V, K, true, false>
+                  <<<grid, kConvThreads, 0, stream>>>(a);
+          }
         });
       });
     });
