@@ -647,3 +647,26 @@ def test_scan_steps_far_apart(t, kind, step):
                                   out=apart(3), **kw)
     for p, q in zip(grads, got):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("t,b,c,k,dtype", [
+    (16, 3, 8, 5, BF16), (17, 2, 7, 5, F32), (40, 3, 7, 5, F16),
+    (150, 2, 130, 5, F32), (150, 16, 1401, 4, BF16), (150, 16, 1401, 1, F32),
+    (300, 16, 1402, 2, F16)])
+@pytest.mark.parametrize("kind", ["", "l", "b", "lb"])
+def test_conv_long_tiles(t, b, c, k, dtype, kind):
+    """Gradients over tiles long enough for steps that test for nothing: their
+    ends, rows that end inside a tile, and the windows."""
+    say(f"[gpu] time conv, long tiles {t} {b} {c} {k} {dtype} {kind!r}")
+    ln, _, rev = axes(kind, t, b)
+    x, w, bias = rnd(171, t, b, c, dtype=dtype), rnd(172, k, c), rnd(173, c)
+    wi = rnd(174, k - 1, b, c, dtype=dtype)
+    dy = rnd(175, t, b, c, dtype=dtype)
+    dwo = rnd(176, k - 1, b, c, dtype=dtype)
+    got = ops.time_conv_backward(dy, x, w, bias, act=2, window=wi,
+                                 lengths=dev(ln), reverse=rev,
+                                 dwindow_out=dwo)
+    want = R.time_conv_backward(f64(dy), f64(x), f64(w), f64(bias), R.SILU,
+                                f64(wi), lengths=ln, reverse=rev,
+                                dwindow_out=f64(dwo))
+    compare(dict(zip(("dx", "dweight", "dbias", "dwindow"), got)), want, "")
