@@ -456,7 +456,9 @@ st_status st_group_norm_workspace(const st_norm_desc* d, int32_t backward,
  * (biased variance) over the group's channels and all sites.  gamma, beta:
  * [c], NULL for 1 and 0.  mean, rstd: [n][groups], written for
  * st_group_norm_backward; both or neither may be NULL.  y may be x itself
- * (the same address, strides and type).
+ * (the same address, strides and type).  An image's results are the same bits
+ * alone and among others (in maps of the same strides and alignment), as is
+ * its dx in the backward call.
  * Errors: ST_ERR_INVALID_ARG, ST_ERR_WORKSPACE, ST_ERR_HIP. */
 st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
                         const float* gamma, const float* beta,

@@ -58,7 +58,7 @@ struct NormArgs {
   float* part;
   float* bases;        // forward: [n][groups], what means are relative to
   int parts;
-  // The images that a launch sums up and those that it finishes.
+  // The images that a launch sums up and those that it finishes (held: all).
   int sum0, sum1, end0, end1;
   float* chpart;       // backward: [n][slabs][c] {sum dz, sum dz xh}
   float* dgamma;
@@ -269,6 +269,17 @@ void with_norm(int dtype, int out_dtype, const NormGeom& g, F&& f) {
 
 inline unsigned pass_blocks(const NormArgs& a) {
   return grid_of((int64_t)(a.end1 - a.end0 + a.sum1 - a.sum0) * a.g.units);
+}
+// Calls f(arguments, blocks) for the launches of blocks that hold whole groups,
+// each over as many images as a grid has room for.
+template <class F>
+void with_held(NormArgs a, F&& f) {
+  const int64_t most = std::max<int64_t>(1, kMaxGrid / a.g.units);
+  for (int64_t i = 0; i < a.g.n; i += most) {
+    a.end0 = (int)i;
+    a.end1 = (int)std::min<int64_t>(i + most, a.g.n);
+    f(a, (unsigned)((int64_t)(a.end1 - a.end0) * a.g.units));
+  }
 }
 // Calls f(arguments, last) for the launches over large images, each of which sums
 // up the images of one batch and finishes those of the batch before: a batch is

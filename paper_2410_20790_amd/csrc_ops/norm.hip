@@ -294,8 +294,8 @@ __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
   const NormGeom& g = a.g;
   __shared__ float res[kMaxCols * S * 3];
   const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  const int u = near_block(g.n * g.units);
-  const Place p = place_of(g, u / g.units, u % g.units);
+  const int u = near_block((a.end1 - a.end0) * g.units);
+  const Place p = place_of(g, a.end0 + u / g.units, u % g.units);
   const bool on = row < g.rows && col < p.nvec;
   const int ch = (p.vec0 + (on ? col : 0)) * V;
   const int left = on ? (int)g.sites - row : 0;   // sites from its own on
@@ -347,15 +347,23 @@ __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
 
 // -------------------------------------------------------------- host side
 
-// Rules of the cut, each with what it measured (us, in a replayed graph).
-// Held blocks take more groups, for whole cache lines, while there is one to a
-// CU: 32 images of 8x8x320 f32 7.4 (8.4 with two to a CU).
-constexpr int kHeldBlocks = 256;
-// Blocks of 256 threads that a batch of images is cut into: four to a CU;
-// 4x61x67x513 f16 29 (34 with eight), others within 1%.
+// Rules of the cut, each with what it measured (us, in a replayed graph).  They
+// follow an image's own sizes, not the number of images: an image's sums are
+// joined in the same order, to the same bits, alone and among others.
+// Held blocks take more groups while a site has less than a cache line of them:
+// 8x8x320 f32 6.1 for one image and 6.4 for 32 (6.5 and 6.9 with two lines);
+// 64x64x256 f16 14.6 and 57 (12.4 and 90 without).
+constexpr int kHeldLine = 128;
+// Blocks of 256 threads that an image is cut into, four to a CU, while their
+// threads have enough to sum up before they join: as many sites, and as many
+// bytes (backward: of x), of vectors that groups or strides keep narrow.  16-byte
+// vectors: 9x32x64x2048 bf16 54 (59 with 8 sites), one such image 16 (14).  One
+// channel to a vector, 61x67x513 f16: four images 28 and one 17 (32 and 15 with
+// half the bytes, 34 and 23 with twice as many); backward 53 and 23 (63 and 22,
+// 48 and 29).
 constexpr int kTargetBlocks = 1024;
+constexpr int kMinSites = 16, kMinBytes = 128, kMinGradBytes = 64;
 constexpr int kMaxEntries = 4096;     // parts of all groups a block joins
-constexpr int kMinSites = 16;         // sites a thread has at least
 // Bytes of a site to a block, two cache lines: 9x256x512x256 bf16 357 (368
 // with four lines, 353 with one, which loses where they are streamed out).
 constexpr int kLine = 256;
@@ -407,22 +415,17 @@ void columns(NormGeom& g, int threads, int units) {
 }
 
 // Blocks that hold an image's groups whole, `held` sites a thread at most.
-bool hold(NormGeom& g, int threads, int held) {
+bool hold(NormGeom& g, int es, int threads, int held) {
   const int mul = g.v / std::gcd(g.cpg, g.v);
   const int unit = g.cpg * mul / g.v;
   if (unit > kMaxCols) return false;
   columns(g, threads, 1);
-  if (ceil_div(g.sites, g.rows) > held ||
-      (int64_t)g.n * g.colblocks > kMaxGrid)
+  if (ceil_div(g.sites, g.rows) > held || g.colblocks > kMaxGrid)
     return false;
-  // wider blocks while there are more than enough: whole cache lines, fewer
-  // of them
   NormGeom w = g;
-  for (int u = 2; u * unit <= kMaxCols; u *= 2) {
+  for (int u = 2; g.cols * g.v * es < kHeldLine && g.colblocks > 1; u *= 2) {
     columns(w, threads, u);
-    if (ceil_div(w.sites, w.rows) > held ||
-        (int64_t)w.n * w.colblocks < kHeldBlocks)
-      break;
+    if (ceil_div(w.sites, w.rows) > held) break;
     g = w;
   }
   g.slabs = 1;
@@ -439,15 +442,16 @@ int batch_of(const NormGeom& g, int es) {
 
 // Blocks that take a range of an image's sites: columns of at least kLine
 // bytes, and no more ranges than a block of the next pass can join.
-void split(NormGeom& g, int es, int batch) {
+void split(NormGeom& g, int es, bool backward) {
   const int mul = g.v / std::gcd(g.cpg, g.v);
   const int unit = g.cpg * mul / g.v;
   columns(g, kThreads, std::max(1, std::min<int>(kMaxCols / unit,
                         (int)ceil_div(kLine, (int64_t)unit * g.v * es))));
-  const int64_t blocks = (int64_t)batch * g.colblocks;
-  const int64_t most =
-      ceil_div(g.sites, (int64_t)g.rows * kMinSites);
-  int64_t slabs = std::min<int64_t>(most, ceil_div(kTargetBlocks, blocks));
+  const int least =
+      std::max(kMinSites, (backward ? kMinGradBytes : kMinBytes) / (g.v * es));
+  const int64_t most = ceil_div(g.sites, (int64_t)g.rows * least);
+  int64_t slabs =
+      std::min<int64_t>(most, ceil_div(kTargetBlocks, g.colblocks));
   slabs = std::min<int64_t>(slabs, kMaxEntries / (g.kg * g.cparts));
   slabs = std::max<int64_t>(1, slabs);
   g.slab_sites = ceil_div(g.sites, slabs);
@@ -457,9 +461,6 @@ void split(NormGeom& g, int es, int batch) {
 
 int read_size(const st_norm_desc& d, bool backward) {
   return esize(d.dtype) + (backward ? esize(d.out_dtype) : 0);
-}
-void split_for(const st_norm_desc& d, NormGeom& g, bool backward) {
-  split(g, esize(d.dtype), batch_of(g, read_size(d, backward)));
 }
 
 struct NormSpace {
@@ -580,10 +581,11 @@ NormMap map_of(const st_norm_desc& d, const st_map_ref& m,
 // backward pass), or 0 and a cut into site ranges.  (8x47x78x512 f16 22 us
 // held, 26 in ranges; 4x64x64x256 f16 15 and 17; 32x8x8x320 f32 8 and 14.)
 int hold_or_split(const st_norm_desc& d, NormGeom& g, bool backward) {
-  if (hold(g, kFewThreads, kHeld)) return kFewThreads;
-  if (hold(g, kManyThreads, backward ? kHeld / 2 : kHeld))
+  const int es = esize(d.dtype);
+  if (hold(g, es, kFewThreads, kHeld)) return kFewThreads;
+  if (hold(g, es, kManyThreads, backward ? kHeld / 2 : kHeld))
     return kManyThreads;
-  split_for(d, g, backward);
+  split(g, es, backward);
   return 0;
 }
 
@@ -619,16 +621,19 @@ st_status check_space(const st_norm_desc& d, bool backward, const void* ws,
 
 void launch_norm(const NormArgs& a, int dtype, int out_dtype, int held,
                  int batch, hipStream_t q) {
-  const unsigned grid = (unsigned)((int64_t)a.g.n * a.g.units);
   with_norm(dtype, out_dtype, a.g, [&](auto ti, auto to, auto vt, auto wt) {
     using T = typename decltype(ti)::type;
     using O = typename decltype(to)::type;
     constexpr int V = decltype(vt)::value;
     constexpr bool W = decltype(wt)::value;
-    if (held == kFewThreads) {
-      k_norm_held<T, O, V, W, kFewThreads><<<grid, kFewThreads, 0, q>>>(a);
-    } else if (held == kManyThreads) {
-      k_norm_held<T, O, V, W, kManyThreads><<<grid, kManyThreads, 0, q>>>(a);
+    if (held) {
+      with_held(a, [&](const NormArgs& b, unsigned grid) {
+        if (held == kFewThreads)
+          k_norm_held<T, O, V, W, kFewThreads><<<grid, kFewThreads, 0, q>>>(b);
+        else
+          k_norm_held<T, O, V, W, kManyThreads>
+              <<<grid, kManyThreads, 0, q>>>(b);
+      });
     } else {
       with_activation(a.act, [&](auto act) {
         with_batches(a, batch, [&](const NormArgs& b, bool) {

@@ -301,8 +301,8 @@ __global__ __launch_bounds__(TH) void k_norm_grad_held(NormArgs a) {
   const NormGeom& g = a.g;
   __shared__ float res[kMaxCols * (WHOLE ? 1 : V) * 2];
   const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
-  const int u = near_block(g.n * g.units);
-  const Place p = place_of(g, u / g.units, u % g.units);
+  const int u = near_block((a.end1 - a.end0) * g.units);
+  const Place p = place_of(g, a.end0 + u / g.units, u % g.units);
   const bool on = row < g.rows && col < p.nvec;
   const int ch = (p.vec0 + (on ? col : 0)) * V;
   const int left = on ? (int)g.sites - row : 0;   // sites from its own on
@@ -362,13 +362,14 @@ void launch_norm_backward(const NormArgs& a, int dtype, int out_dtype,
     constexpr int V = decltype(vt)::value;
     constexpr bool W = decltype(wt)::value;
     if (held) {
-      const unsigned grid = (unsigned)(a.g.n * a.g.units);
-      if (held == kFewThreads)
-        k_norm_grad_held<T, O, V, W, kFewThreads, kHeld>
-            <<<grid, kFewThreads, 0, q>>>(a);
-      else
-        k_norm_grad_held<T, O, V, W, kManyThreads, kHeld / 2>
-            <<<grid, kManyThreads, 0, q>>>(a);
+      with_held(a, [&](const NormArgs& b, unsigned grid) {
+        if (held == kFewThreads)
+          k_norm_grad_held<T, O, V, W, kFewThreads, kHeld>
+              <<<grid, kFewThreads, 0, q>>>(b);
+        else
+          k_norm_grad_held<T, O, V, W, kManyThreads, kHeld / 2>
+              <<<grid, kManyThreads, 0, q>>>(b);
+      });
       if (a.dblocks) k_norm_channels<<<a.dblocks, kThreads, 0, q>>>(a);
       return;
     }

@@ -670,3 +670,28 @@ def test_conv_long_tiles(t, b, c, k, dtype, kind):
                                 f64(wi), lengths=ln, reverse=rev,
                                 dwindow_out=f64(dwo))
     compare(dict(zip(("dx", "dweight", "dbias", "dwindow"), got)), want, "")
+
+
+@pytest.mark.parametrize("shape,groups,pair", [
+    # held in registers, with groups of a few channels
+    ((32, 8, 8, 320), 32, (F32, F32)), ((300, 2, 2, 16), 4, (F32, BF16)),
+    ((16, 64, 64, 256), 32, (F16, F16)),
+    # summed up in parts
+    ((9, 128, 128, 256), 32, (F32, F32)), ((32, 32, 64, 512), 1, (F32, F32)),
+    ((5, 61, 67, 513), 27, (F16, F16)), ((9, 64, 128, 512), 32, (BF16, BF16)),
+    ((7, 60, 80, 258), 2, (F32, F16))])
+def test_norm_images_apart(shape, groups, pair):
+    """An image alone and among others: the same bits, forward and back."""
+    say(f"[gpu] group norm, images apart {shape} / {groups} {pair}")
+    x, dy = rnd(181, *shape, dtype=pair[0]), rnd(182, *shape, dtype=pair[1])
+    g, b = rnd(183, shape[-1], shift=1.0), rnd(184, shape[-1])
+    y, m, r = ops.group_norm(x, groups, g, b, act=2, out_dtype=pair[1])
+    dx = ops.group_norm_backward(dy, x, groups, m, r, g, b, act=2)[0]
+    k = shape[0] // 2
+    for s in (slice(0, 1), slice(k, k + 1), slice(k, k + 3), slice(-1, None)):
+        got = ops.group_norm(x[s], groups, g, b, act=2, out_dtype=pair[1])
+        for p, q in zip(got, (y, m, r)):
+            assert torch.equal(p, q[s])
+        got = ops.group_norm_backward(dy[s], x[s], groups, m[s], r[s], g, b,
+                                      act=2)[0]
+        assert torch.equal(got, dx[s])

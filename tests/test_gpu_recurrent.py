@@ -177,3 +177,18 @@ def test_refusals():
         head.forward(torch.zeros(2, 1, 3, 3, 24, device="cuda"),
                      head.new_state(8))
     net.close()
+
+
+def test_head_over_frames_equals_the_chunk():
+    """The head's outputs for a chunk and for its frames, on maps whose norm
+    is summed up in parts: the same bits, and the same memory."""
+    say("[gpu] recurrent head, frames and chunk")
+    t, n, hh, w, c = 6, 2, 64, 64, 512
+    head = make_head(c, groups=32)
+    g = torch.Generator().manual_seed(21)
+    feats = torch.randn(t, n, hh, w, 3 * c, generator=g).cuda()
+    a, b = head.new_state(n * hh * w), head.new_state(n * hh * w)
+    y = head.forward(feats, a)
+    for i in range(t):
+        assert torch.equal(head.forward(feats[i:i + 1], b)[0], y[i])
+    assert torch.equal(a.h, b.h) and torch.equal(a.window, b.window)
