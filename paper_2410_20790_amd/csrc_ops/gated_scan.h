@@ -61,6 +61,15 @@ __device__ __forceinline__ void then(float& A, float& H, float x, float y) {
   H = cut ? y : __builtin_fmaf(x, H, y);
   A = cut ? x : A * x;
 }
+// A product of gates none of which is zero (nor a cut) does not become zero,
+// however many they are: an infinite state passes them, as it passes one after
+// another.  (Seen to once for many factors, where the product is zero.)
+__device__ __forceinline__ bool is_zero(float A) {
+  return __float_as_uint(A) == 0;
+}
+__device__ __forceinline__ void keep_product(float& A, bool zero_factor) {
+  if (is_zero(A) && !zero_factor) A = 0x1p-149f;
+}
 // The state after the steps of (A, H), from the state h.
 __device__ __forceinline__ float after(float A, float H, float h) {
   return is_cut(A) ? H : __builtin_fmaf(A, h, H);
@@ -93,6 +102,7 @@ struct Ends {
 __device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
                                              float& A, float& H) {
   constexpr int N = 4;
+  bool zero = false;
   const Word* q = p.at(i0);
   for (int i = i0; i < i1; i += N) {
     Word w[N];
@@ -110,12 +120,15 @@ __device__ __forceinline__ void fold_entries(const Ends& p, int i0, int i1,
     for (int k = 0; k < N; ++k) {
       if (i + k < i1) {
         const uint32_t hi = (uint32_t)(w[k] >> 32);
-        then(A, H, hi == kCutBits ? kCut : __uint_as_float(hi & 0x7fffffffu),
-             __uint_as_float((uint32_t)w[k]));
+        const float x =
+            hi == kCutBits ? kCut : __uint_as_float(hi & 0x7fffffffu);
+        then(A, H, x, __uint_as_float((uint32_t)w[k]));
+        zero = zero || is_zero(x);
       }
     }
     q += N * p.plane;
   }
+  keep_product(A, zero);
 }
 
 // A block's lanes and waves, in running order: wave 0 has the first steps to
@@ -146,6 +159,15 @@ __device__ __forceinline__ void join_waves(TileShared<W>& sh, int wave,
       H = TH;
     }
     then(TA, TH, sh.a[w][at], sh.h[w][at]);
+  }
+  if (__any(is_zero(A) || is_zero(TA))) {
+    bool zero = false;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w == wave) keep_product(A, zero);
+      zero = zero || is_zero(sh.a[w][at]);
+    }
+    keep_product(TA, zero);
   }
 }
 
@@ -182,6 +204,7 @@ __device__ __forceinline__ void enter_tile(const ScanArgs& a,
     A = PA;
     H = PH;
     then(A, H, TA, TH);
+    keep_product(A, is_zero(PA) || is_zero(TA));
     publish(p.at((int64_t)a.tiles + g), A, H);
   }
   // the groups before its own

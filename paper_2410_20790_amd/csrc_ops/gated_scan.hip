@@ -133,6 +133,12 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
         A *= keep[k];
       }
     }
+    if (__any(is_zero(A))) {
+      bool zero = false;
+#pragma unroll
+      for (int k = 0; k < kSplit; ++k) zero = zero || is_zero(keep[k]);
+      keep_product(A, zero);
+    }
   }
   if (tile == 0) arrived(h);
   join_waves(sh, wave, A, H, TA, TH);

@@ -87,6 +87,12 @@ struct GradSteps {
       D = cut ? 0.f : (D + g[k]) * keep[k];
       A = cut ? kCut : A * keep[k];
     }
+    if (__any(is_zero(A))) {
+      bool zero = false;
+#pragma unroll
+      for (int k = 0; k < kSplit; ++k) zero = zero || is_zero(keep[k]);
+      keep_product(A, zero);
+    }
   }
 
   // dv and df; dh becomes what goes on to the step before.

@@ -695,3 +695,28 @@ def test_norm_images_apart(shape, groups, pair):
         got = ops.group_norm_backward(dy[s], x[s], groups, m[s], r[s], g, b,
                                       act=2)[0]
         assert torch.equal(got, dx[s])
+
+
+@pytest.mark.parametrize("t", [20, 700, 9000])
+@pytest.mark.parametrize("f0", [-30.0, 0.0, 4.0])
+def test_scan_infinite_states(t, f0):
+    """An infinite state stays infinite behind gates that are not zero, in
+    short rows and in rows split along time, however small the product of the
+    gates; so does an infinite gradient on its way back."""
+    say(f"[gpu] gated scan, infinite states {t} {f0}")
+    b, c = 2, 8
+    v, dy = rnd(191, t, b, c), rnd(192, t, b, c)
+    f, o = rnd(193, t, b, c, shift=f0), rnd(194, t, b, c)
+    h, dh = rnd(195, b, c), rnd(196, b, c)
+    h[0, 1], v[t // 3, 1, 2] = float("inf"), -float("inf")
+    dh[0, 3], dy[t // 2, 1, 4] = -float("inf"), float("inf")
+    y, ho, st = ops.gated_scan(v, f, o, h=h, save=True)
+    want = R.gated_scan(f64(v), f64(f), f64(o), f64(h))
+    want.pop("states")
+    compare(dict(y=y, h=ho), want, "infinite")
+    v[t // 3, 1, 2], h[0, 1] = 0.0, 0.0
+    st = ops.gated_scan(v, f, o, h=h, save=True)[2]
+    got = ops.gated_scan_backward(dy, v, f, o, states=st, dh=dh)
+    compare(dict(zip(("dv", "df", "do", "dh"), got)),
+            R.gated_scan_backward(f64(dy), f64(v), f64(f), f64(o), f64(h),
+                                  dh=f64(dh)), "infinite, back")
