@@ -38,6 +38,13 @@ def _code(x, name):
     return code
 
 
+def _fits(*values):
+    """Refuses what the library's 32-bit integers cannot hold: ctypes would
+    wrap it."""
+    if max(values) > 0x7fffffff or min(values) < -0x80000000:
+        raise ValueError("sizes, groups and activations must lie below 2^31")
+
+
 def _mismatch(name, shape, dtype, device, contiguous=False):
     return ValueError(
         f"{name} must be a {'contiguous ' if contiguous else ''}tensor "
@@ -132,6 +139,7 @@ def _norm_desc(x, groups, act, eps, out_dtype):
     _require(x.dim() in (3, 4),
              "x must be [n, h, w, c] or [n, sites, c]")
     s = x.shape
+    _fits(*s, groups, act)
     h, w = (s[1], s[2]) if len(s) == 4 else (s[1], 1)
     return B.st_norm_desc(code, _CODES[out_dtype], s[0], h, w, s[-1], groups,
                           act, eps)
@@ -208,10 +216,11 @@ def _seq(x, shape, device, name, dtype=None):
     return B.st_seq_ref(x.data_ptr(), st[0], st[1])
 
 
-def _seq_desc(x, out_dtype, lengths, reset, reverse):
+def _seq_desc(x, out_dtype, lengths, reset, reverse, act=0):
     code = _code(x, "the input")
     _require(x.dim() == 3, "sequences are [t, b, c]")
     t, b, c = x.shape
+    _fits(t, b, c, act)
     ln = _plain(lengths, (b,), torch.int32, x.device, "lengths")
     if reset is not None and reset.dtype == torch.bool:
         reset = reset.view(torch.uint8)
@@ -229,7 +238,7 @@ def time_conv(x, weight, bias=None, act=0, window=None, lengths=None,
     [taps - 1, b, c] of x's type (zeros if absent).  window_out, the window
     of the next call over the same rows, may be window itself."""
     dt = _out_dtype(x, out, out_dtype)
-    d = _seq_desc(x, dt, lengths, reset, reverse)
+    d = _seq_desc(x, dt, lengths, reset, reverse, act)
     dev, (t, b, c) = x.device, x.shape
     _require(weight.dim() == 2 and
              1 <= weight.shape[0] <= B.TIME_CONV_MAX_TAPS,
@@ -262,7 +271,7 @@ def time_conv_backward(dy, x, weight, bias=None, act=0, window=None,
     dwindow_out: the gradient with respect to window_out (zero if absent)."""
     _code(dy, "dy")
     dt = _out_dtype(x, None, dy.dtype)
-    d = _seq_desc(x, dt, lengths, reset, reverse)
+    d = _seq_desc(x, dt, lengths, reset, reverse, act)
     dev, (t, b, c) = x.device, x.shape
     _require(weight.dim() == 2 and
              1 <= weight.shape[0] <= B.TIME_CONV_MAX_TAPS,

@@ -267,3 +267,30 @@ def test_maps_larger_than_any_memory():
         d = norm_desc(n=1, h=h, w=w, c=c, groups=1)
         for back in (0, 1):
             refused(BAD, "2^40", B.st_group_norm_workspace, d, back)
+
+
+@pytest.mark.parametrize("far", [2 ** 31, 2 ** 32 + 5, 2 ** 33 + 2])
+def test_sizes_beyond_32_bits(far, monkeypatch):
+    """What the descriptors' integers would wrap is refused, not taken for a
+    small size (tensors without memory in place of device tensors)."""
+    monkeypatch.setattr(ops, "_code", lambda x, name: 0)
+
+    def t(*shape):
+        return torch.empty(shape, device="meta")
+    for call in (lambda: ops.group_norm(t(1, far, 1), 1),
+                 lambda: ops.group_norm(t(far, 2, 2, 4), 2),
+                 lambda: ops.group_norm(t(1, 2, far, 4), 2),
+                 lambda: ops.group_norm(t(1, 2, 2, 4), far),
+                 lambda: ops.group_norm(t(1, 2, 2, 4), 2, act=far),
+                 lambda: ops.group_norm_backward(
+                     t(1, far, 1), t(1, far, 1), 1, t(1, 1), t(1, 1)),
+                 lambda: ops.time_conv(t(far, 1, 1), t(3, 1)),
+                 lambda: ops.time_conv(t(2, 1, 1), t(3, 1), act=far),
+                 lambda: ops.time_conv_backward(t(2, far, 1), t(2, far, 1),
+                                                t(3, 1)),
+                 lambda: ops.gated_scan(t(far, 1, 1), t(far, 1, 1)),
+                 lambda: ops.gated_scan_backward(
+                     t(far, 1, 1), t(far, 1, 1), t(far, 1, 1),
+                     states=t(1, 1, 1))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
