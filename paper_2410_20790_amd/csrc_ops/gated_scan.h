@@ -253,7 +253,8 @@ __device__ __forceinline__ int next_ticket(const ScanArgs& a,
   return __builtin_amdgcn_readfirstlane(sh.ticket);
 }
 // N steps of a tensor from step s0 on; for those that the row does not have,
-// whatever it has last.  whole: all lanes of the wave have all of them.
+// whatever it has last, or zero if it has none of them: behind its length a row
+// is not read, and need not be there.  whole: all lanes of the wave have all.
 template <int N, bool NARROW, typename T, int V>
 __device__ __forceinline__ void load_steps(const SeqTensor& x,
                                            const ScanArgs& a, const Row& r,
@@ -261,13 +262,18 @@ __device__ __forceinline__ void load_steps(const SeqTensor& x,
                                            Pack<T, V>* out) {
   StepsAt<const T, NARROW> p(x, a.q, r, b, ch, s0);
   if (!whole) {
+    if (s0 < r.len) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      out[k] = load_pack<T, V>(p.here());
-      p.next(k);
-      // (keeps these loads apart from those below: the compiler would form all
-      // addresses in registers first and load in one place)
-      __builtin_amdgcn_sched_barrier(0);
+      for (int k = 0; k < N; ++k) {
+        out[k] = load_pack<T, V>(p.here());
+        p.next(k);
+        // (keeps these loads apart from those below: the compiler would form
+        // all addresses in registers first and load in one place)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) out[k] = Pack<T, V>{};
     }
   } else if (a.stream) {
 #pragma unroll
@@ -282,7 +288,7 @@ template <int N, bool NARROW>
 __device__ __forceinline__ unsigned cuts_of(const ScanArgs& a, const Row& r,
                                             int b, int s0) {
   unsigned m = 0;
-  if (a.q.reset) {
+  if (a.q.reset && s0 < r.len) {
     // all loads at once: none waits for another
     const SeqTensor t{(void*)a.q.reset, a.q.b, 1};
     StepsAt<const uint8_t, NARROW> p(t, a.q, r, b, 0, s0);

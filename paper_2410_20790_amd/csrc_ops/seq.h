@@ -46,9 +46,9 @@ __device__ __forceinline__ bool reset_at(const SeqAxes& q, const Row& r,
 }
 
 // A row's elements in running order, from step s0 on: next() goes to the next
-// step, or stays where the row ends (an address that may be read, time 0 of a
-// row of no steps).  One addition per step; the products that a time and its
-// stride make up are formed once.  NARROW: offsets of 32 bits into the tensor.
+// step, or stays where the row ends.  One addition per step; the products that
+// a time and its stride make up are formed once.  NARROW: offsets of 32 bits
+// into the tensor.
 template <typename T, bool NARROW>
 struct Walk {
   typedef std::conditional_t<NARROW, uint32_t, int64_t> Off;
@@ -116,7 +116,8 @@ struct StepsAt {
   __device__ __forceinline__ T* at(int k) const {
     return (T*)(p + k * step + off);
   }
-  // The same one by one: on to the next step, or to where the row ends.
+  // The same one by one, of a row that has step s0: on to the next step, or to
+  // where the row ends.
   __device__ __forceinline__ T* here() const { return (T*)(p + off); }
   __device__ __forceinline__ void next(int k) {     // from step s0 + k
     off += k < left ? (Off)step : 0;

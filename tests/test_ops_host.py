@@ -2,12 +2,14 @@
 host: every call here returns before anything is launched."""
 
 import ctypes
+import os
+import subprocess
 
 import pytest
 import torch
 
 from paper_2410_20790_amd import binding as B
-from paper_2410_20790_amd import ops
+from paper_2410_20790_amd import build, ops
 
 A = 1 << 20            # addresses nothing is read from
 BAD, SMALL = B.ST_ERR_INVALID_ARG, B.ST_ERR_WORKSPACE
@@ -294,3 +296,16 @@ def test_sizes_beyond_32_bits(far, monkeypatch):
                      states=t(1, 1, 1))):
         with pytest.raises(ValueError, match="2\\^31"):
             call()
+
+
+def test_padding_need_not_be_there(tmp_path):
+    """The recurrence's loads, compiled for the host: nothing behind a row's
+    length is read, at any step of rows that end before it."""
+    exe = str(tmp_path / "padding_reads")
+    src = os.path.join(os.path.dirname(__file__), "padding_reads.hip")
+    subprocess.run([build.HIPCC, "-x", "hip", f"--offload-arch={build.ARCH}",
+                    "--offload-host-only", "-O1", "-std=c++17",
+                    "-I", build.OPS, src, "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.endswith("ok\n"), (
+        r.returncode, r.stdout[-200:])
