@@ -53,10 +53,9 @@ struct NormArgs {
   float eps;
   int act;
   // Large images: parts of a group's sums, one for each range of sites (and
-  // part of a group); forward [n][groups][parts] {count, mean, M2}, backward
-  // {sum dz gamma, sum dz gamma xh}
+  // part of a group); forward [n][groups][parts] {count, mean in two
+  // parts, M2}, backward {sum dz gamma, sum dz gamma xh}
   float* part;
-  float* bases;        // forward: [n][groups], what means are relative to
   int parts;
   // The images that a launch sums up and those that it finishes (held: all).
   int sum0, sum1, end0, end1;
@@ -198,6 +197,13 @@ template <typename F>
 __device__ __forceinline__ F lanes_sum(F x, int lanes) {
   for (int d = lanes >> 1; d; d >>= 1) x += __shfl_xor(x, d);
   return x;
+}
+__device__ __forceinline__ void lanes_sum2(float& x, float& y, int lanes) {
+  for (int d = lanes >> 1; d; d >>= 1) {
+    const float a = __shfl_xor(x, d), b = __shfl_xor(y, d);
+    x += a;
+    y += b;
+  }
 }
 // Places of a block's entries of one group: `wide` adjacent ones of every row,
 // `lanes` apart, each lane from its own on.

@@ -17,8 +17,9 @@ namespace {
 constexpr int kBatch = 4, kSumBatch = 8;
 
 // Adds a batch of M values to (cnt, mean, m2): the batch's own mean first,
-// then its squared deviations from that mean.  Values come relative to one
-// value of their group: a mean far from zero costs no digits.
+// then its squared deviations from that mean.  Values come relative to the
+// thread's first: a mean far from zero costs no digits, and a value far from the
+// others costs those of its own thread alone.
 template <int M>
 __device__ __forceinline__ void add_batch(const float* f, float& cnt,
                                           float& mean, float& m2) {
@@ -39,13 +40,6 @@ __device__ __forceinline__ void add_batch(const float* f, float& cnt,
   cnt = n;
 }
 
-// The value of a group that its values are taken relative to: the first
-// channel of the first site.
-template <typename T>
-__device__ __forceinline__ float base_of(const NormArgs& a, int n, int gr) {
-  return to_f(((const T*)a.x.p)[n * a.x.sn + (int64_t)gr * a.g.cpg]);
-}
-
 // The moments of a vector of values, or (not WHOLE) of each of its channels.
 template <int V, bool WHOLE>
 struct Moments {
@@ -55,11 +49,14 @@ struct Moments {
 #pragma unroll
     for (int i = 0; i < S; ++i) base[i] = cnt[i] = mean[i] = m2[i] = 0.f;
   }
+  // The base: what the thread has first.
   template <typename T>
-  __device__ __forceinline__ void set_base(const NormArgs& a, int n, int ch) {
+  __device__ __forceinline__ void begin(const Pack<T, V>& first) {
 #pragma unroll
-    for (int i = 0; i < S; ++i)
-      base[i] = base_of<T>(a, n, (ch + i) / a.g.cpg);
+    for (int i = 0; i < S; ++i) {
+      const float x = to_f(first.e[i]);
+      if (cnt[i] == 0.f && __builtin_fabsf(x) < __builtin_inff()) base[i] = x;
+    }
   }
   template <typename T, int N>
   __device__ __forceinline__ void add(const Pack<T, V>* r) {
@@ -84,21 +81,40 @@ struct Moments {
   }
 };
 
-// Joins the block's moments: group j of the block ends at out[3 j] (count,
-// mean, squared deviations), for all its threads.  Means first, then the
-// deviations from the joint mean, over the lanes that share a group.
+// The mean and the squared deviations of values whose distances from `near`, a
+// value not far from their mean, add up to `rest` over the lanes, and the squares
+// of these (beside deviations of their own) to `q`.
+struct Joined {
+  float mean, left, m2;    // left: what the mean's rounding left
+  __device__ __forceinline__ Joined(float near, float rest, float q, float inv,
+                                    int lanes) {
+    lanes_sum2(rest, q, lanes);
+    const float d = rest * inv;
+    const bool finite = __builtin_fabsf(near) < __builtin_inff();
+    mean = finite ? near + d : near;
+    left = finite ? d - (mean - near) : 0.f;
+    q -= rest * d;
+    m2 = q < 0.f ? 0.f : q;    // NaN stays
+  }
+};
+
+// Joins the block's moments: group j of the block ends at out[4 j] (count, mean
+// in two parts, squared deviations), for all its threads, over the lanes that
+// share a group.  The mean of the threads' means comes first, as the roundings
+// leave it; relative to it, what they left out, and the deviations.
 template <int V, bool WHOLE, int TH>
 __device__ __forceinline__ void block_moments(const NormGeom& g,
                                               const Place& p,
                                               const Moments<V, WHOLE>& m,
                                               float* out) {
   constexpr int S = WHOLE ? 1 : V;
-  __shared__ float sc[TH * S], sm[TH * S], sq[TH * S];
+  __shared__ float sc[TH * S], sb[TH * S], sm[TH * S], sq[TH * S];
   const int tid = threadIdx.x;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < S; ++i) {
     sc[tid * S + i] = m.cnt[i];
+    sb[tid * S + i] = m.base[i];
     sm[tid * S + i] = m.mean[i];
     sq[tid * S + i] = m.m2[i];
   }
@@ -108,24 +124,26 @@ __device__ __forceinline__ void block_moments(const NormGeom& g,
   const Entries first(in, lanes, wide);
   const float n = (float)(p.s1 - p.s0) *
                   (float)(g.cparts == 1 ? g.cpg : p.nvec * V);
+  const float inv = 1.f / n;
   for (int j = tid / lanes; j < p.ng; j += TH / lanes) {
-    float q = 0.f;
-    double s = 0;   // (its values need not be near zero)
+    float s = 0.f, rest = 0.f, q = 0.f;
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
-      s += (double)sc[at] * sm[at];
+      s += sc[at] * (sb[at] + sm[at]);
     }
-    const float mean = (float)lanes_sum(s, lanes) / n;
+    const float near = lanes_sum(s, lanes) * inv;
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
-      const float d = sm[at] - mean;
-      q += sq[at] + sc[at] * d * d;   // (no values: count and mean are zero)
+      const float c = sc[at], d = sb[at] - near + sm[at];
+      rest += c * d;    // (no values: all are zero)
+      q += sq[at] + c * d * d;
     }
-    q = lanes_sum(q, lanes);
+    const Joined r(near, rest, q, inv, lanes);
     if (in == 0) {
-      out[j * 3] = n;
-      out[j * 3 + 1] = mean;
-      out[j * 3 + 2] = q;
+      out[j * 4] = n;
+      out[j * 4 + 1] = r.mean;
+      out[j * 4 + 2] = r.left;
+      out[j * 4 + 3] = r.m2;
     }
   }
   __syncthreads();
@@ -140,7 +158,6 @@ __device__ __forceinline__ void stats_unit(const NormArgs& a, const Place& p,
   Moments<V, WHOLE> m;
   if (row < g.rows && col < p.nvec) {
     const int ch = (p.vec0 + col) * V;
-    m.template set_base<T>(a, p.n, ch);
     int64_t s = p.s0 + row;
     SiteWalk<const T> x(a.x, p.n, s, ch);
     Pack<T, V> r[kSumBatch];
@@ -150,26 +167,22 @@ __device__ __forceinline__ void stats_unit(const NormArgs& a, const Place& p,
         r[k] = load_pack<T, V>(x.p);
         x.next();
       }
+      m.begin(r[0]);
       m.template add<T, kSumBatch>(r);
     }
     for (; s < p.s1; s += g.rows) {
       r[0] = load_pack<T, V>(x.p);
       x.next();
+      m.begin(r[0]);
       m.template add<T, 1>(r);
     }
   }
   block_moments<V, WHOLE, kThreads>(g, p, m, res);
   const int part = p.slab * g.cparts + p.cb % g.cparts;
   for (int j = threadIdx.x; j < p.ng; j += kThreads) {
-    float* o = a.part +
-               (((int64_t)p.n * g.groups + p.g0 + j) * a.parts + part) * 3;
-    o[0] = res[j * 3];
-    o[1] = res[j * 3 + 1];
-    o[2] = res[j * 3 + 2];
-    // kept: y may take x's place before all blocks have read it there
-    if (part == 0)
-      a.bases[(int64_t)p.n * g.groups + p.g0 + j] =
-          base_of<T>(a, p.n, p.g0 + j);
+    ((float4*)a.part)[((int64_t)p.n * g.groups + p.g0 + j) * a.parts + part] =
+        make_float4(res[j * 4], res[j * 4 + 1], res[j * 4 + 2],
+                    res[j * 4 + 3]);
   }
 }
 
@@ -180,32 +193,29 @@ __device__ __forceinline__ void join_parts(const NormArgs& a, const Place& p,
   const NormGeom& g = a.g;
   const int lanes = lanes_per_group(kThreads, p.ng);
   const int in = threadIdx.x & (lanes - 1);
+  const float n = (float)((double)g.sites * g.cpg), inv = 1.f / n;
   for (int j = threadIdx.x / lanes; j < p.ng; j += kThreads / lanes) {
     const int64_t at = (int64_t)p.n * g.groups + p.g0 + j;
-    const float* part = a.part + at * a.parts * 3;
-    float q = 0.f;
-    double n = 0, s = 0;
+    const float4* part = (const float4*)a.part + at * a.parts;
+    // A part of n of the group's M values whose mean a value D carries off is D
+    // / n away, the group's deviation D / sqrt(M) or more: near enough, with
+    // hundreds of values in a part and about as many parts.
+    const float near = part[0].y;
+    float rest = 0.f, q = 0.f;
 #pragma unroll 4
     for (int i = in; i < a.parts; i += lanes) {
-      n += part[i * 3];
-      s += (double)part[i * 3] * part[i * 3 + 1];
+      const float4 o = part[i];
+      const float d = o.y - near + o.z;
+      rest += o.x * d;
+      q += o.w + o.x * d * d;
     }
-    n = lanes_sum(n, lanes);
-    const double md = lanes_sum(s, lanes) / n;
-    const float m = (float)md;
-#pragma unroll 4
-    for (int i = in; i < a.parts; i += lanes) {
-      const float d = part[i * 3 + 1] - m;
-      q += part[i * 3 + 2] + part[i * 3] * d * d;
-    }
-    q = lanes_sum(q, lanes);
-    const float mean = (float)(a.bases[at] + md);
-    const float rstd = 1.f / sqrtf(q / (float)n + a.eps);
+    const Joined r(near, rest, q, inv, lanes);
+    const float rstd = 1.f / sqrtf(r.m2 / n + a.eps);
     if (in == 0) {
-      res[j * 2] = mean;
+      res[j * 2] = r.mean;
       res[j * 2 + 1] = rstd;
       if (a.mean_out && p.slab == 0 && p.cb % g.cparts == 0) {
-        a.mean_out[at] = mean;
+        a.mean_out[at] = r.mean;
         a.rstd_out[at] = rstd;
       }
     }
@@ -272,7 +282,7 @@ __device__ __forceinline__ void apply_unit(const NormArgs& a, const Place& p,
 // [sum0, sum1), in turn, so that reads and writes mix.
 template <typename T, typename O, int V, bool WHOLE, int ACT>
 __global__ __launch_bounds__(kThreads) void k_norm_pass(NormArgs a) {
-  __shared__ float res[kMaxCols * (WHOLE ? 1 : V) * 3];
+  __shared__ float res[kMaxCols * (WHOLE ? 1 : V) * 4];
   const int ends = (a.end1 - a.end0) * a.g.units;
   const int all = ends + (a.sum1 - a.sum0) * a.g.units;
   for (int b = blockIdx.x; b < all; b += gridDim.x) {
@@ -292,7 +302,7 @@ template <typename T, typename O, int V, bool WHOLE, int TH>
 __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
   constexpr int S = WHOLE ? 1 : V;
   const NormGeom& g = a.g;
-  __shared__ float res[kMaxCols * S * 3];
+  __shared__ float res[kMaxCols * S * 4];
   const int col = threadIdx.x % g.cols, row = threadIdx.x / g.cols;
   const int u = near_block((a.end1 - a.end0) * g.units);
   const Place p = place_of(g, a.end0 + u / g.units, u % g.units);
@@ -307,30 +317,25 @@ __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
     x.next();
   }
   Moments<V, WHOLE> m;
-  m.template set_base<T>(a, p.n, ch);
   Params<V, WHOLE> q;
   q.load_affine(a, ch);
-  const float jbase = base_of<T>(a, p.n, min(p.g0 + (int)threadIdx.x,
-                                             g.groups - 1));
+  if (left > 0) m.begin(r[0]);
 #pragma unroll
   for (int k = 0; k < kHeld; ++k)
     if (k * g.rows < left) m.template add<T, 1>(r + k);
   block_moments<V, WHOLE, TH>(g, p, m, res);
   for (int j = threadIdx.x; j < p.ng; j += TH) {
-    const float mean =
-        (j < TH ? jbase : base_of<T>(a, p.n, p.g0 + j)) + res[j * 3 + 1];
-    const float rstd = 1.f / sqrtf(res[j * 3 + 2] / res[j * 3] + a.eps);
-    res[j * 3] = mean;
-    res[j * 3 + 1] = rstd;
+    const float rstd = 1.f / sqrtf(res[j * 4 + 3] / res[j * 4] + a.eps);
+    res[j * 4 + 2] = rstd;
     if (a.mean_out) {
       const int64_t at = (int64_t)p.n * g.groups + p.g0 + j;
-      a.mean_out[at] = mean;
+      a.mean_out[at] = res[j * 4 + 1];
       a.rstd_out[at] = rstd;
     }
   }
   __syncthreads();
   float scale[V];
-  q.load_stats(res, 3, ch, g.cpg, p.g0);
+  q.load_stats(res + 1, 4, ch, g.cpg, p.g0);
 #pragma unroll
   for (int i = 0; i < V; ++i) scale[i] = q.r(i) * q.gamma[i];
   SiteWalk<O> y(a.y, p.n, row, ch);
@@ -464,7 +469,7 @@ int read_size(const st_norm_desc& d, bool backward) {
 }
 
 struct NormSpace {
-  size_t part = 0, bases = 0, chpart = 0, bytes = 0;
+  size_t part = 0, chpart = 0, bytes = 0;
 };
 NormSpace space_of(const NormGeom& g, bool backward, int held) {
   NormSpace s;
@@ -476,11 +481,8 @@ NormSpace space_of(const NormGeom& g, bool backward, int held) {
   };
   if (!held)
     s.part = take((int64_t)g.n * g.groups * g.slabs * g.cparts *
-                  (backward ? 2 : 3));
-  if (backward)
-    s.chpart = take((int64_t)g.n * g.slabs * g.c * 2);
-  else if (!held)
-    s.bases = take((int64_t)g.n * g.groups);
+                  (backward ? 2 : 4));
+  if (backward) s.chpart = take((int64_t)g.n * g.slabs * g.c * 2);
   s.bytes = top;
   return s;
 }
@@ -702,7 +704,6 @@ extern "C" st_status st_group_norm(const st_norm_desc* d, const st_map_ref* x,
     a.beta = beta;
     a.eps = d->eps;
     a.part = (float*)(w + sp.part);
-    a.bases = (float*)(w + sp.bases);
     a.parts = a.g.slabs * a.g.cparts;
     a.mean_out = mean;
     a.rstd_out = rstd;

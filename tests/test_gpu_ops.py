@@ -720,3 +720,31 @@ def test_scan_infinite_states(t, f0):
     compare(dict(zip(("dv", "df", "do", "dh"), got)),
             R.gated_scan_backward(f64(dy), f64(v), f64(f), f64(o), f64(h),
                                   dh=f64(dh)), "infinite, back")
+
+
+@pytest.mark.parametrize("shape,groups", [
+    ((1, 8, 8, 16), 1), ((2, 64, 64, 32), 2), ((1, 512, 256, 32), 1),
+    ((1, 300, 200, 33), 3)])
+@pytest.mark.parametrize("at", [(0, 0, 0), (-1, -1, -1)])
+def test_norm_one_value_far_out(shape, groups, at):
+    """A flat background with one bright value, the first or the last of the
+    image: it costs the others no digits.  Of the background x, y = (x - mean)
+    rstd within: U |mean| rstd for the mean's rounding, 2 U |y|, and 16 U of a
+    deviation for what the sums carry (a thread that holds the bright value D
+    loses U D of each of its others, less than one in sqrt(M) of a group's M
+    values, whose deviation is D / sqrt(M) or more)."""
+    say(f"[gpu] group norm, one value far out {shape} / {groups} {at}")
+    x = torch.full(shape, 0.1, device="cuda")
+    x[0][at] = 1e4
+    eps = 1e-5      # groups without the bright value are all of one value
+    y, mean, rstd = ops.group_norm(x, groups, eps=eps)
+    want = R.group_norm(f64(x), groups, None, None, R.NONE, eps)
+    n, c = shape[0], shape[-1]
+    m, r = (np.broadcast_to(want[k][0][:, None, None, :, None],
+                            (n, 1, 1, groups, c // groups)).reshape(
+                                n, 1, 1, c) for k in ("mean", "rstd"))
+    w = want["y"][0]
+    check(y, w, 16 * R.U + R.U * (2 * np.abs(m) * r + 18 * np.abs(w)),
+          "far out")
+    check(mean, want["mean"][0], 16 * R.U / want["rstd"][0], "mean")
+    check(rstd, want["rstd"][0], 18 * R.U * want["rstd"][0], "rstd")
