@@ -6,7 +6,9 @@ include/sparsetem.h for what each computes).
 The functions check the tensors, allocate outputs and workspace from torch,
 and pass addresses and the current stream of the tensors' device to the
 library.  No computation happens here, and no autograd graph is recorded:
-the backward calls are the gradients.
+the backward calls are the gradients.  Where torch would record one -- a
+tensor requires a gradient, outside torch.no_grad() and the methods of a
+torch.autograd.Function -- a call is refused, not cut off in silence.
 
 Maps are [n, ..., c] with one or two axes of sites, or views of such; sequences
 are [t, b, c].  Channels are adjacent in memory, other strides are free.
@@ -52,6 +54,14 @@ def _mismatch(name, shape, dtype, device, contiguous=False):
         f"{device}")
 
 
+def _no_graph(name):
+    if torch.is_grad_enabled():
+        raise ValueError(
+            f"{name} requires a gradient, which the operators do not record: "
+            f"call them under torch.no_grad() or in a torch.autograd.Function, "
+            f"with their backward calls, or detach it")
+
+
 def _plain(x, shape, dtype, device, name):
     """Address of a contiguous tensor that may be absent."""
     if x is None:
@@ -63,6 +73,8 @@ def _plain(x, shape, dtype, device, name):
         good = False
     if not good:
         raise _mismatch(name, shape, dtype, device, True)
+    if x.requires_grad:
+        _no_graph(name)
     return x.data_ptr()
 
 
@@ -129,6 +141,8 @@ def _map(x, shape, device, name, dtype=None):
         raise _mismatch(name, shape, dtype, device)
     if st[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name}: channels must be adjacent")
+    if x.requires_grad:
+        _no_graph(name)
     if len(shape) == 4:
         return B.st_map_ref(x.data_ptr(), st[0], st[1], st[2])
     return B.st_map_ref(x.data_ptr(), st[0], st[1], st[1])
@@ -213,6 +227,8 @@ def _seq(x, shape, device, name, dtype=None):
         raise _mismatch(name, shape, dtype, device)
     if st[2] != 1 and shape[2] != 1:
         raise ValueError(f"{name}: channels must be adjacent")
+    if x.requires_grad:
+        _no_graph(name)
     return B.st_seq_ref(x.data_ptr(), st[0], st[1])
 
 

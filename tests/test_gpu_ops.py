@@ -748,3 +748,36 @@ def test_norm_one_value_far_out(shape, groups, at):
           "far out")
     check(mean, want["mean"][0], 16 * R.U / want["rstd"][0], "mean")
     check(rstd, want["rstd"][0], 18 * R.U * want["rstd"][0], "rstd")
+
+
+def test_gradients_recorded_by_the_caller():
+    """Inputs that require gradients: refused where torch records, taken under
+    no_grad and in an autograd function, whose gradients are the backward
+    calls'."""
+    say("[gpu] gradients recorded by the caller")
+    v, f, o, dy = (rnd(200 + i, 20, 3, 8) for i in range(4))
+
+    class Scan(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, *x):
+            y, _, st = ops.gated_scan(*x, save=True)
+            ctx.save_for_backward(*x, st)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            *x, st = ctx.saved_tensors
+            return ops.gated_scan_backward(dy, *x, states=st)[:3]
+
+    want, _, st = ops.gated_scan(v, f, o, save=True)
+    grads = ops.gated_scan_backward(dy, v, f, o, states=st)
+    leaves = [q.clone().requires_grad_() for q in (v, f, o)]
+    with pytest.raises(ValueError, match="requires a gradient"):
+        ops.gated_scan(*leaves)
+    with torch.no_grad():
+        assert torch.equal(ops.gated_scan(*leaves)[0], want)
+    y = Scan.apply(*leaves)
+    assert torch.equal(y, want)
+    y.backward(dy)
+    for q, g in zip(leaves, grads):
+        assert torch.equal(q.grad, g)

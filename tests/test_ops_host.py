@@ -309,3 +309,35 @@ def test_padding_need_not_be_there(tmp_path):
     r = subprocess.run([exe], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.endswith("ok\n"), (
         r.returncode, r.stdout[-200:])
+
+
+def _calls(grad, t):
+    """(name, call) of every operator with one input that requires a
+    gradient; t makes a tensor, grad one that requires it."""
+    x4, p, st = t(1, 2, 2, 4), t(4), t(1, 2)
+    x, w, h = t(3, 2, 4), t(3, 4), t(2, 4)
+    kept = t(1, 2, 4)
+    return [
+        ("x", lambda: ops.group_norm(grad(x4), 2)),
+        ("gamma", lambda: ops.group_norm(x4, 2, grad(p))),
+        ("beta", lambda: ops.group_norm(x4, 2, p, grad(p))),
+        ("dy", lambda: ops.group_norm_backward(grad(x4), x4, 2, st, st)),
+        ("x", lambda: ops.time_conv(grad(x), w)),
+        ("weight", lambda: ops.time_conv(x, grad(w))),
+        ("window", lambda: ops.time_conv(x, w, window=grad(t(2, 2, 4)))),
+        ("weight", lambda: ops.time_conv_backward(x, x, grad(w))),
+        ("v", lambda: ops.gated_scan(grad(x), x)),
+        ("f", lambda: ops.gated_scan(x, grad(x))),
+        ("o", lambda: ops.gated_scan(x, x, grad(x))),
+        ("h", lambda: ops.gated_scan(x, x, h=grad(h))),
+        ("dh", lambda: ops.gated_scan_backward(x, x, x, states=kept,
+                                               dh=grad(h)))]
+
+
+def test_gradients_that_nothing_would_record(monkeypatch):
+    """An input that requires a gradient is refused where torch records."""
+    monkeypatch.setattr(ops, "_code", lambda x, name: 0)
+    for name, call in _calls(lambda x: x.clone().requires_grad_(),
+                             lambda *s: torch.empty(s, device="meta")):
+        with pytest.raises(ValueError, match=f"^{name} requires a gradient"):
+            call()
