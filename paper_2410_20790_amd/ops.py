@@ -40,11 +40,12 @@ def _code(x, name):
     return code
 
 
-def _fits(*values):
-    """Refuses what the library's 32-bit integers cannot hold: ctypes would
-    wrap it."""
-    if max(values) > 0x7fffffff or min(values) < -0x80000000:
-        raise ValueError("sizes, groups and activations must lie below 2^31")
+# what the library's 32-bit integers hold: ctypes would wrap the rest
+_MOST = 0x7fffffff
+
+
+def _too_large():
+    return ValueError("sizes, groups and activations must lie below 2^31")
 
 
 def _mismatch(name, shape, dtype, device, contiguous=False):
@@ -153,8 +154,10 @@ def _norm_desc(x, groups, act, eps, out_dtype):
     _require(x.dim() in (3, 4),
              "x must be [n, h, w, c] or [n, sites, c]")
     s = x.shape
-    _fits(*s, groups, act)
     h, w = (s[1], s[2]) if len(s) == 4 else (s[1], 1)
+    if not (s[0] <= _MOST and h <= _MOST and w <= _MOST and s[-1] <= _MOST
+            and -_MOST <= groups <= _MOST and -_MOST <= act <= _MOST):
+        raise _too_large()
     return B.st_norm_desc(code, _CODES[out_dtype], s[0], h, w, s[-1], groups,
                           act, eps)
 
@@ -236,7 +239,9 @@ def _seq_desc(x, out_dtype, lengths, reset, reverse, act=0):
     code = _code(x, "the input")
     _require(x.dim() == 3, "sequences are [t, b, c]")
     t, b, c = x.shape
-    _fits(t, b, c, act)
+    if not (t <= _MOST and b <= _MOST and c <= _MOST
+            and -_MOST <= act <= _MOST):
+        raise _too_large()
     ln = _plain(lengths, (b,), torch.int32, x.device, "lengths")
     if reset is not None and reset.dtype == torch.bool:
         reset = reset.view(torch.uint8)
