@@ -13,6 +13,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import binding as B
 from . import ops
 from .net import SparseTemNet
 
@@ -47,6 +48,12 @@ class RecurrentHead:
         if channels < 1 or taps < 1 or groups < 1 or channels % groups:
             raise ValueError("channels and taps must be positive, and groups "
                              "must divide the channels")
+        if taps > B.TIME_CONV_MAX_TAPS:
+            raise ValueError(f"taps must not exceed {B.TIME_CONV_MAX_TAPS}")
+        if act not in (0, 1, 2):
+            raise ValueError("act must be 0 (none), 1 (ReLU) or 2 (SiLU)")
+        if not 0 <= eps < float("inf"):
+            raise ValueError("eps must be finite and not negative")
         self.channels, self.taps, self.groups = channels, taps, groups
         self.act, self.eps = act, eps
         dev = torch.device(device)
@@ -75,12 +82,25 @@ class RecurrentHead:
         seq = feats.reshape(t, n * h * w, 3 * c)
         return seq[..., :c], seq[..., c:2 * c], seq[..., 2 * c:]
 
+    def _check(self, feats, state):
+        """What the operators would refuse once the first of them has moved
+        the window on."""
+        t, n, h, w, _ = feats.shape
+        c, dev, f32 = self.channels, self.weight.device, torch.float32
+        ops._plain(state.window, (self.taps - 1, n * h * w, c), feats.dtype,
+                   dev, "window")
+        ops._plain(state.h, (n * h * w, c), f32, dev, "h")
+        ops._plain(self.gamma, (c,), f32, dev, "gamma")
+        ops._plain(self.beta, (c,), f32, dev, "beta")
+
     def forward(self, feats, state: HeadState, reset=None, save=False):
         """y [t, n, h, w, c] of the maps feats [t, n, h, w, 3 c]; `state`
-        moves on in place.  reset: uint8 [t, rows], non-zero where a row
-        forgets the frames before (a cut).  With save: (y, Saved)."""
+        moves on in place (a call that is refused leaves it as it was).
+        reset: uint8 [t, rows], non-zero where a row forgets the frames before
+        (a cut).  With save: (y, Saved)."""
         v, f, o = self._split(feats)
         t, n, h, w, _ = feats.shape
+        self._check(feats, state)
         before = state.window.clone() if save else None
         u, _ = ops.time_conv(v, self.weight, self.bias, act=2,
                              window=state.window, window_out=state.window,

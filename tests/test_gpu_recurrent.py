@@ -192,3 +192,32 @@ def test_head_over_frames_equals_the_chunk():
     for i in range(t):
         assert torch.equal(head.forward(feats[i:i + 1], b)[0], y[i])
     assert torch.equal(a.h, b.h) and torch.equal(a.window, b.window)
+
+
+def test_refused_calls_leave_the_memory():
+    """A call that is refused, by whichever of the head's operators, leaves
+    the window and the state as they were; parameters that no call takes are
+    refused when the head is made."""
+    say("[gpu] recurrent head, refused calls")
+    for kw in (dict(taps=9), dict(act=3), dict(act=-1), dict(eps=-1e-5),
+               dict(eps=float("nan")), dict(eps=float("inf"))):
+        with pytest.raises(ValueError):
+            RecurrentHead(8, **kw)
+    g = torch.Generator().manual_seed(22)
+    feats = torch.randn(2, 1, 3, 3, 24, generator=g).cuda()
+    spoil = [("gamma", torch.ones(7, device="cuda")),
+             ("beta", torch.ones(8)),
+             ("gamma", torch.ones(8, device="cuda", requires_grad=True))]
+    for name, value in [("h", None)] + spoil:
+        head = make_head(8)
+        st = head.new_state(9)
+        head.forward(feats, st)
+        keep = [q.clone() for q in st]
+        if name == "h":
+            given = st._replace(h=st.h[:, :4])
+        else:
+            given = st
+            setattr(head, name, value)
+        with pytest.raises(ValueError):
+            head.forward(feats, given)
+        assert torch.equal(st.window, keep[0]) and torch.equal(st.h, keep[1])
