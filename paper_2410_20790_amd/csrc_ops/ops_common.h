@@ -101,12 +101,12 @@ __device__ __forceinline__ float sigmoid_once(float x) {
 }
 
 // sigmoid(x) and sigmoid(-x) likewise.  (n as e p rather than 1 - p, whose
-// error a large factor would magnify; where e is that large p is next to zero,
-// and so is every result.)
+// error a large factor would magnify; beyond 2^126, where p is no normal number
+// any more, every result is zero.)
 __device__ __forceinline__ void sigmoids_once(float x, float& p, float& n) {
   const float e = __builtin_amdgcn_exp2f(x * -1.44269502162933349609f);
   p = __builtin_amdgcn_rcpf(1.f + e);
-  n = fminf(e, 0x1p100f) * p;
+  n = fminf(e, 0x1p126f) * p;
 }
 
 // f(z) and its derivative for the activation ACT (ST_ACT_*).

@@ -781,3 +781,24 @@ def test_gradients_recorded_by_the_caller():
     y.backward(dy)
     for q, g in zip(leaves, grads):
         assert torch.equal(q.grad, g)
+
+
+def test_gradients_of_closed_gates():
+    """Output gates and SiLU far below zero, whose factors are small but normal
+    numbers: gradients within their bound relative to themselves."""
+    say("[gpu] gradients of closed gates")
+    t, b, c = 24, 2, 8
+    far = torch.linspace(-86.0, -40.0, t, device="cuda")[:, None, None]
+    o = far.expand(t, b, c).contiguous()
+    v, f, dy = rnd(221, t, b, c), rnd(222, t, b, c), rnd(223, t, b, c)
+    st = ops.gated_scan(v, f, o, save=True)[2]
+    got = ops.gated_scan_backward(dy, v, f, o, states=st)
+    want = R.gated_scan_backward(f64(dy), f64(v), f64(f), f64(o))
+    w, bound = want["do"]
+    # its two factors, the sigmoid and its exponent's rounding
+    check(got[2], w, bound + 2 * R.once(f64(o)) * np.abs(w), "do")
+    one = torch.ones(1, c, device="cuda")
+    dx = ops.time_conv_backward(dy, o, one, act=2, need_params=False)[0]
+    z = f64(o)
+    w = f64(dy) * R.dact(z, R.SILU)
+    check(dx, w, 4 * R.once(z) * np.abs(w), "SiLU")
