@@ -429,7 +429,10 @@ st_status st_profile_end(st_net* net, st_launch_record* recs, int32_t cap,
  * ST_F32 with any; `dtype` is that of the inputs and of their gradients,
  * `out_dtype` that of the output and of its gradient.  Parameters,
  * statistics and the recurrent state are f32, and so is all arithmetic;
- * results are rounded once, to nearest even. */
+ * results are rounded once, to nearest even.  A sigmoid that scales a value
+ * (SiLU, the output gate, their derivatives) is within (4 + 1.25 |x|) 2^-24 of
+ * itself, one that a state is carried by (the forget gate) within 8 * 2^-24,
+ * relative. */
 
 /* A channels-last map [n][h][w][c]: strides in elements, channels adjacent.
  * An output's elements must not overlap. */

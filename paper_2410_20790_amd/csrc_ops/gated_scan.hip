@@ -158,15 +158,14 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
     auto gated = [&](int k) {
       return GATE ? h * sigmoid_once(to_f(io[k].e[0])) : h;
     };
+    const StepsAt<O, NARROW> y(a.y, a.q, r, l.b, l.ch, s0);
     if (whole && !cutting) {
-      const StepsAt<O, NARROW> y(a.y, a.q, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         h = __builtin_fmaf(keep[k], h, u[k]);
         *y.at(k) = from_f<O>(gated(k));
       }
     } else {
-      const StepsAt<O, NARROW> y(a.y, a.q, r, l.b, l.ch, s0);
 #pragma unroll
       for (int k = 0; k < kSplit; ++k) {
         if (s0 + k < r.len) {

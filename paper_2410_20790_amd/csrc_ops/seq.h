@@ -109,7 +109,9 @@ struct StepsAt {
     step = q.reverse ? -x.st * es : x.st * es;
     off = (Off)(at * es);
     // (formed anew wherever it is used: across blocks the compiler would keep
-    // it added to the address, two registers for every load in flight)
+    // it added to the address, two registers for every load in flight.  Walked
+    // rows form one in each branch for that: above the branch, 300 steps of 600
+    // rows of 512 channels bf16 take 186 us for 166)
     if constexpr (NARROW) asm volatile("" : "+v"(off));
   }
   // Step s0 + k, which the row must have.
