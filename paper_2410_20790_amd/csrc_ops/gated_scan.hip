@@ -101,8 +101,9 @@ __global__ __launch_bounds__(64 * W) void k_scan_tiles(ScanArgs a) {
   if (any) {
     cuts = cuts_of<kSplit, NARROW>(a, r, l.b, s0);
     Pack<T, 1> iv[kSplit], jf[kSplit];
-    // (one branch over all loads: with one in each, 100 steps of 300 rows of 256
-    // channels take 11% more; the backward pass, of more loads, takes 10% less)
+    // (one branch over all loads: with one in each, 100 steps of 300 rows of
+    // 256 channels take 11% more; the backward pass, of more loads, takes up to
+    // 10% less)
     if (s0 < r.len) {
       load_steps<kSplit, NARROW>(a.f, a, r, l.b, l.ch, s0, whole, jf);
       load_steps<kSplit, NARROW>(a.v, a, r, l.b, l.ch, s0, whole, iv);

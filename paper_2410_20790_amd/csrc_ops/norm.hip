@@ -18,8 +18,8 @@ constexpr int kBatch = 4, kSumBatch = 8;
 
 // Adds a batch of M values to (cnt, mean, m2): the batch's own mean first,
 // then its squared deviations from that mean.  Values come relative to the
-// thread's first: a mean far from zero costs no digits, and a value far from the
-// others costs those of its own thread alone.
+// thread's first: a mean far from zero costs no digits, and a value far from
+// the others costs those of its own thread alone.
 template <int M>
 __device__ __forceinline__ void add_batch(const float* f, float& cnt,
                                           float& mean, float& m2) {
@@ -82,8 +82,8 @@ struct Moments {
 };
 
 // The mean and the squared deviations of values whose distances from `near`, a
-// value not far from their mean, add up to `rest` over the lanes, and the squares
-// of these (beside deviations of their own) to `q`.
+// value not far from their mean, add up to `rest` over the lanes, and the
+// squares of these (beside deviations of their own) to `q`.
 struct Joined {
   float mean, left, m2;    // left: what the mean's rounding left
   __device__ __forceinline__ Joined(float near, float rest, float q, float inv,
@@ -356,16 +356,16 @@ __global__ __launch_bounds__(TH) void k_norm_held(NormArgs a) {
 // follow an image's own sizes, not the number of images: an image's sums are
 // joined in the same order, to the same bits, alone and among others.
 // Held blocks take more groups while a site has less than a cache line of them:
-// 8x8x320 f32 6.1 for one image and 6.4 for 32 (6.5 and 6.9 with two lines);
-// 64x64x256 f16 14.6 and 57 (12.4 and 90 without).
+// 8x8x320 f32 6.2 for one image and 6.6 for 32 (half a us more with two lines);
+// 64x64x256 f16 14 and 57 (12.4 and 90 without).
 constexpr int kHeldLine = 128;
 // Blocks of 256 threads that an image is cut into, four to a CU, while their
 // threads have enough to sum up before they join: as many sites, and as many
-// bytes (backward: of x), of vectors that groups or strides keep narrow.  16-byte
-// vectors: 9x32x64x2048 bf16 54 (59 with 8 sites), one such image 16 (14).  One
-// channel to a vector, 61x67x513 f16: four images 28 and one 17 (32 and 15 with
-// half the bytes, 34 and 23 with twice as many); backward 53 and 23 (63 and 22,
-// 48 and 29).
+// bytes (backward: of x), of vectors that groups or strides keep narrow.
+// 16-byte vectors: 9x32x64x2048 bf16 54 (59 with 8 sites), one such image 16
+// (14).  One channel to a vector, 61x67x513 f16: four images 28 and one 17 (32
+// and 15 with half the bytes, 34 and 23 with twice as many); backward 53 and 23
+// (63 and 22, 48 and 29).
 constexpr int kTargetBlocks = 1024;
 constexpr int kMinSites = 16, kMinBytes = 128, kMinGradBytes = 64;
 constexpr int kMaxEntries = 4096;     // parts of all groups a block joins
@@ -580,8 +580,9 @@ NormMap map_of(const st_norm_desc& d, const st_map_ref& m,
   return r;
 }
 // The threads of the blocks that hold the image's groups (of x and dy in the
-// backward pass), or 0 and a cut into site ranges.  (8x47x78x512 f16 22 us
-// held, 26 in ranges; 4x64x64x256 f16 15 and 17; 32x8x8x320 f32 8 and 14.)
+// backward pass), or 0 and a cut into site ranges.  (8x47x78x512 f16 20.5 us
+// held, 23 in ranges; 16x64x64x256 f16 21 and 22.5, one such image 14 and 14.5;
+// 32x8x8x320 f32 6.6 and 11; 9x32x64x512 f32 in 32 groups 27 and 25.)
 int hold_or_split(const st_norm_desc& d, NormGeom& g, bool backward) {
   const int es = esize(d.dtype);
   if (hold(g, es, kFewThreads, kHeld)) return kFewThreads;

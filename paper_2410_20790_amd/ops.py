@@ -59,8 +59,8 @@ def _no_graph(name):
     if torch.is_grad_enabled():
         raise ValueError(
             f"{name} requires a gradient, which the operators do not record: "
-            f"call them under torch.no_grad() or in a torch.autograd.Function, "
-            f"with their backward calls, or detach it")
+            "call them under torch.no_grad() or in a torch.autograd.Function "
+            "with their backward calls, or detach it")
 
 
 def _plain(x, shape, dtype, device, name):
