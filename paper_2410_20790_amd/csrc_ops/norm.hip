@@ -364,8 +364,9 @@ constexpr int kHeldLine = 128;
 // bytes (backward: of x), of vectors that groups or strides keep narrow.
 // 16-byte vectors: 9x32x64x2048 bf16 54 (59 with 8 sites), one such image 16
 // (14).  One channel to a vector, 61x67x513 f16: four images 28 and one 17 (32
-// and 15 with half the bytes, 34 and 23 with twice as many); backward 53 and 23
-// (63 and 22, 48 and 29).
+// and 15 with half the bytes, 34 and 23 with twice as many); backward 41 and 23
+// (46 and 21 with half the bytes); one channel of 67, backward: nine images of
+// 200x300 bf16 133 (167 with half, 125 with twice as many), one 29 (29 and 36).
 constexpr int kTargetBlocks = 1024;
 constexpr int kMinSites = 16, kMinBytes = 128, kMinGradBytes = 64;
 constexpr int kMaxEntries = 4096;     // parts of all groups a block joins
@@ -450,8 +451,15 @@ int batch_of(const NormGeom& g, int es) {
 void split(NormGeom& g, int es, bool backward) {
   const int mul = g.v / std::gcd(g.cpg, g.v);
   const int unit = g.cpg * mul / g.v;
-  columns(g, kThreads, std::max(1, std::min<int>(kMaxCols / unit,
-                        (int)ceil_div(kLine, (int64_t)unit * g.v * es))));
+  const int units =
+      std::min<int>(kMaxCols / unit,
+                    (int)ceil_div(kLine, (int64_t)unit * g.v * es));
+  columns(g, kThreads, std::max(1, units));
+  // Backward, a second row of columns rather than threads without any:
+  // 4x61x67x513 f16, 133 columns or 114, 41 us (53); forward 28 (26).
+  constexpr int kHalf = kThreads / 2;
+  if (backward && g.cols > kHalf && g.cols * 4 < kThreads * 3 && unit <= kHalf)
+    columns(g, kThreads, kHalf / unit);
   const int least =
       std::max(kMinSites, (backward ? kMinGradBytes : kMinBytes) / (g.v * es));
   const int64_t most = ceil_div(g.sites, (int64_t)g.rows * least);
