@@ -802,3 +802,31 @@ def test_gradients_of_closed_gates():
     z = f64(o)
     w = f64(dy) * R.dact(z, R.SILU)
     check(dx, w, 4 * R.once(z) * np.abs(w), "SiLU")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [9, 70])
+def test_sequences_into_slices(t, dtype):
+    """Outputs written into slices of a wider tensor, rows before time, with
+    zeros behind the rows' ends; the rest of it stays."""
+    say(f"[gpu] sequences into slices {t} {dtype}")
+    b, c = 5, 10
+    ln, rs, _ = axes("lr", t, b)
+    x, f, w = rnd(231, t, b, c, dtype=dtype), rnd(232, t, b, c,
+                                                  dtype=dtype), rnd(233, 4, c)
+    for rev in (False, True):
+        kw = dict(lengths=dev(ln), reset=dev(rs), reverse=rev)
+        room = torch.full((b, t, 3 * c + 3), 7.0, dtype=dtype, device="cuda")
+        wide = room.transpose(0, 1)
+        for at, call in ((1, lambda o: ops.time_conv(x, w, act=2, out=o,
+                                                     **kw)[0]),
+                         (c + 2, lambda o: ops.gated_scan(x, f, x, out=o,
+                                                          **kw)[0])):
+            want = call(None)
+            got = call(wide[..., at:at + c])
+            assert torch.equal(got, want)
+            live = torch.arange(t)[:, None] < torch.from_numpy(
+                np.clip(ln, 0, t))[None]
+            assert (got[~live.cuda()] == 0).all()
+        assert (room[..., 0] == 7).all() and (room[..., c + 1] == 7).all()
+        assert (room[..., 2 * c + 2:] == 7).all()

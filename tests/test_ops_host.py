@@ -2,14 +2,12 @@
 host: every call here returns before anything is launched."""
 
 import ctypes
-import os
-import subprocess
 
 import pytest
 import torch
 
 from paper_2410_20790_amd import binding as B
-from paper_2410_20790_amd import build, ops
+from paper_2410_20790_amd import ops
 
 A = 1 << 20            # addresses nothing is read from
 BAD, SMALL = B.ST_ERR_INVALID_ARG, B.ST_ERR_WORKSPACE
@@ -301,6 +299,10 @@ def test_sizes_beyond_32_bits(far, monkeypatch):
 def test_padding_need_not_be_there(tmp_path):
     """The recurrence's loads, compiled for the host: nothing behind a row's
     length is read, at any step of rows that end before it."""
+    import os
+    import subprocess
+
+    from paper_2410_20790_amd import build
     exe = str(tmp_path / "padding_reads")
     src = os.path.join(os.path.dirname(__file__), "padding_reads.hip")
     subprocess.run([build.HIPCC, "-x", "hip", f"--offload-arch={build.ARCH}",
