@@ -129,9 +129,9 @@ __device__ __forceinline__ void block_moments(const NormGeom& g,
     float s = 0.f, rest = 0.f, q = 0.f;
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
-      s += sc[at] * (sb[at] + sm[at]);
+      s += sc[at] * inv * (sb[at] + sm[at]);   // (no sum beyond its values)
     }
-    const float near = lanes_sum(s, lanes) * inv;
+    const float near = lanes_sum(s, lanes);
     for (Entries e = first; e.row < g.rows; e.next()) {
       const int at = e.row * g.cols * S + j * wide + e.c;
       const float c = sc[at], d = sb[at] - near + sm[at];

@@ -830,3 +830,18 @@ def test_sequences_into_slices(t, dtype):
             assert (got[~live.cuda()] == 0).all()
         assert (room[..., 0] == 7).all() and (room[..., c + 1] == 7).all()
         assert (room[..., 2 * c + 2:] == 7).all()
+
+
+@pytest.mark.parametrize("shape", [(2, 8, 8, 16), (1, 200, 300, 32)])
+def test_norm_of_large_values(shape):
+    """One value throughout, as large as f32 holds with room for a difference:
+    its own mean, no deviation, whatever its sums would reach."""
+    say(f"[gpu] group norm, large values {shape}")
+    beta = rnd(241, shape[-1])
+    for v in (1e37, -1.5e38):
+        x = torch.full(shape, v, device="cuda")
+        y, mean, rstd = ops.group_norm(x, 2, None, beta)
+        assert (mean == x[0, 0, 0, 0]).all()
+        assert (y == beta).all()
+        check(rstd, *R.group_norm(np.zeros(shape), 2, None, None, R.NONE,
+                                  1e-5)["rstd"], "rstd")
