@@ -158,3 +158,32 @@ def test_scan_beyond_the_caches(t, b, c, dtype, kind):
                                      dh=f64(dh[rows, cs]), **k3)
         compare({n: a[..., rows, cs] for n, a in
                  zip(("dv", "df", "do", "dh"), back)}, want, "beyond, back")
+
+
+def test_norm_of_more_images_than_a_grid():
+    """Tiny images, more than one launch has blocks for."""
+    say("[gpu] group norm of more images than a grid")
+    n, c, groups = (1 << 20) + 70001, 8, 2
+    x, dy = big(241, n, 1, 2, c), big(242, n, 1, 2, c)
+    gm, bt = rnd(243, c, shift=1.0), rnd(244, c)
+    y, mean, rstd = ops.group_norm(x, groups, gm, bt, act=2)
+    dx, dg, db = ops.group_norm_backward(dy, x, groups, mean, rstd, gm, bt,
+                                         act=2)
+    for s in (slice(0, 500), slice((1 << 20) - 300, (1 << 20) + 300),
+              slice(n - 500, n)):
+        want = R.group_norm(f64(x[s]), groups, f64(gm), f64(bt), R.SILU, 1e-5)
+        compare(dict(y=y[s], mean=mean[s], rstd=rstd[s]), want, "images")
+        want = R.group_norm_backward(
+            f64(dy[s]), f64(x[s]), groups, f64(mean[s]), f64(rstd[s]),
+            f64(gm), f64(bt), R.SILU)
+        compare(dict(dx=dx[s]), want, "images, back")
+    # the parameters' gradients, in f64 on the device
+    m, r = (q.double().repeat_interleave(c // groups, 1)[:, None, None]
+            for q in (mean, rstd))
+    xh = (x.double() - m) * r
+    z = xh * gm.double() + bt.double()
+    p = torch.sigmoid(z)
+    dz = dy.double() * p * (1 + z * (1 - p))
+    for got, v in ((dg, dz * xh), (db, dz)):
+        err = (got.double() - v.sum((0, 1, 2))).abs()
+        assert (err <= 16 * R.U * v.abs().sum((0, 1, 2))).all()
